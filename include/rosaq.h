@@ -55,6 +55,7 @@ typedef struct rosaq_ctx rosaq_ctx;           /* per device: workspace + device 
 typedef struct rosaq_weight rosaq_weight;     /* one quantized linear in the kernels' tiled layout */
 typedef struct rosaq_rotation rosaq_rotation; /* one rotation R prepared for online use */
 typedef struct rosaq_plan rosaq_plan;         /* a list of rotations / linears that runs as one launch */
+typedef struct rosaq_rope rosaq_rope;         /* rotary positions: frequencies and layout (host memory only) */
 
 /*
  * Description of a rotation R (Section 3.1, Eq. 4; head-wise: Section 3.1.1, Eq. 6).
@@ -348,6 +349,119 @@ int rosaq_plan_schedule(int n_ops, const int32_t *n_tiles, const int32_t *groups
  */
 int rosaq_linear_static(rosaq_ctx *ctx, const void *x, int M, int64_t ldx, const rosaq_rotation *r,
                         const rosaq_weight *w, void *y, int64_t ldy, void *stream);
+
+/* ---- between the q/k/v linears and the o_proj rotation: positions, cache, attention ------------------------
+ *
+ * The linears of a decoder layer above leave these to the caller in the paper; they are here so that a decoding step need not leave the
+ * library.  Rows are fp16, one per token, heads next to each other (what rosaq_linear writes and rosaq_rotate reads); row strides in
+ * elements, multiples of 8; pointers 16-byte aligned.  A call of no rows does nothing and returns ROSAQ_OK.
+ * What the DEVICE arrays of a batch say can only be checked on the device: rows, lengths and pages that do not fit are cut or left out so
+ * that no access leaves the buffers, the status word becomes ROSAQ_ERR_INVALID_ARG (rosaq_last_status), and the results of the
+ * sequences concerned are undefined.
+ */
+
+typedef enum {
+  ROSAQ_ROPE_PLAIN = 0,    /* f_i = base^(-2 i / rot_dim), i < rot_dim / 2 */
+  ROSAQ_ROPE_LINEAR = 1,   /* f_i / factor (positions interpolated) */
+  ROSAQ_ROPE_NTK = 2,      /* base replaced by base * factor^(rot_dim / (rot_dim - 2)); rot_dim >= 4 */
+  ROSAQ_ROPE_BY_PARTS = 3  /* with n_i = context f_i / (2 pi) turns over the original context and w = clamp((n_i - low) / (high - low), 0, 1):
+                            * f_i (w + (1 - w) / factor), i.e. fast pairs as they are, slow ones interpolated */
+} rosaq_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;
+  int32_t rot_dim;         /* even, 2 ... min(head_dim, 256): channels [0, rot_dim) of a head turn, the others are copied */
+  int32_t interleaved;     /* 0: channel i turns with i + rot_dim / 2;  1: 2 i with 2 i + 1 */
+  int32_t scaling;         /* rosaq_rope_scaling */
+  double base, factor, low, high, context;   /* factor > 0 unless plain; low, high, context by parts only */
+  float magnitude;         /* multiplies the channels that turn (1: plain) */
+} rosaq_rope_desc;
+
+/* Works out the frequencies, on the host.  Allocates host memory only; the handle may be used with any context. */
+int rosaq_rope_create(rosaq_ctx *ctx, const rosaq_rope_desc *desc, rosaq_rope **out);
+int rosaq_rope_free(rosaq_rope *r);
+
+/*
+ * y[n_rows][ldy] = the n_heads heads of every row of x[n_rows][ldx] turned by the row's position: with t = positions[row] f_i,
+ *   a' = magnitude (a cos t - b sin t),  b' = magnitude (b cos t + a sin t)   for the pairs (a, b), fp32, rounded once to fp16.
+ *   positions  DEVICE int32 [n_rows]; any value, a negative one turns back.  The angle is exact to 2^-33 turns for all of them.
+ *   y          may be x (same stride); any other overlap is ROSAQ_ERR_INVALID_ARG
+ * q and k next to each other in one buffer are one call.
+ */
+int rosaq_rope_apply(rosaq_ctx *ctx, const rosaq_rope *r, const void *x, int n_rows, int64_t ldx, int n_heads, const int32_t *positions,
+                     void *y, int64_t ldy, void *stream);
+
+/*
+ * A paged cache of keys and values at 4 or 8 bits.  Pages are the caller's memory (any contents at first); a page holds page_tokens tokens of one
+ * sequence, keys and values of all heads.  One group per token and head: with lo and hi the least and the greatest of its head_dim values,
+ *   s = fp16((hi - lo) / (2^bits - 1)), a zero replaced by the smallest subnormal;  code = clamp(rint((x - lo) / s), 0, 2^bits - 1), IEEE fp32, ties to
+ *   even;  the value held is lo + s code.
+ * Infinities are taken as +-65504, NaNs as the least of the other values (a head of nothing but NaNs as zeros).
+ * Inside a page: [head][page_tokens / 16] blocks of 16 tokens; a block is the key codes (2 head_dim bits bytes), the value codes, 16 pairs {s, lo} of the
+ * keys, 16 pairs of the values.  Lane 4 r + c (r < 8, c < 4) has the 32-bit words w < head_dim bits / 64, word w at byte 512 (w / 4) + 16 lane + 4 (w % 4)
+ * of the codes; for h, p, b in {0, 1}:
+ *   4 bits, keys    token 8 h + r,       channel 16 w + 8 p + 2 c + b:   byte 2 b + h of the word, nibble p
+ *   4 bits, values  token 8 h + 2 c + b, channel 16 w + 8 p + r:         byte 2 b + h, nibble p
+ *   8 bits, keys    token 8 h + r,       channel 16 (w / 2) + 8 p + 2 c + b, h = w % 2:   byte 2 p + b
+ *   8 bits, values  token 8 h + 2 c + b, channel 16 (w / 2) + 8 p + r, p = w % 2:         byte 2 h + b
+ */
+typedef struct {
+  void *pages;             /* DEVICE, 16-byte aligned: n_pages pages of rosaq_kv_page_bytes each */
+  int32_t n_pages;
+  int32_t page_tokens;     /* 16, 32, 64, 128, 256, 512 or 1024 */
+  int32_t n_kv_heads;
+  int32_t head_dim;        /* 64 or 128 */
+  int32_t bits;            /* 4 or 8 */
+} rosaq_kv;
+
+/* Bytes of a page, or a negative status. */
+int64_t rosaq_kv_page_bytes(int n_kv_heads, int head_dim, int bits, int page_tokens);
+
+/*
+ * The sequences of a call.  All arrays are DEVICE int32 and read when the launch runs, so a captured call follows their contents.
+ *   row_start  [n_seqs + 1], must ascend: rows [row_start[i], row_start[i + 1]) of the row buffers are the new tokens of sequence i (none: nothing
+ *              happens to it); rows from row_start[n_seqs] on are neither read nor written
+ *   kv_len     [n_seqs] tokens of sequence i in the cache, the new ones included: they are its last ones
+ *   table      [n_seqs][ld_table] pages of sequence i; token t lies in page table[i][t / page_tokens]
+ *   prefix_table, prefix_tokens (HOST number; 0: none)   rosaq_attend: the pages of prefix_tokens further tokens that stand before every
+ *              sequence; they are read once for the whole batch.  kv_len and table do not count them.
+ */
+typedef struct {
+  int32_t n_seqs;
+  int32_t ld_table;        /* ld_table * page_tokens <= 2^30 */
+  const int32_t *row_start, *kv_len, *table;
+  const int32_t *prefix_table;
+  int32_t prefix_tokens;
+} rosaq_kv_batch;
+
+/* Test hook, host only (no GPU, no context; `pages` is not read): where rosaq_kv_write, rosaq_kv_read and rosaq_attend find things for a batch whose three arrays lie
+ * in HOST memory.  Writes, for every row of [0, n_rows), the byte offset in `pages` of the block of head 0 that holds it and its position
+ * (0 ... 15) in it to offset and slot, -1 where the row has no place (it belongs to no sequence, or what the batch says does not fit).
+ * Returns ROSAQ_OK, ROSAQ_ERR_INVALID_ARG when something did not fit (what the calls above put into the status word), or another status. */
+int rosaq_kv_locate(const rosaq_kv *kv, const rosaq_kv_batch *batch, int n_rows, int64_t *offset, int32_t *slot);
+
+/* Quantizes the new rows k[n_rows][ldk], v[n_rows][ldv] (fp16, n_kv_heads heads) into the cache.  Nothing else in the pages changes.  Sequences that share
+ * a page must not write to it in one call.  k and v must not lie in the pages. */
+int rosaq_kv_write(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                   int n_rows, void *stream);
+
+/* Reads the values of the same rows back: the last row_start[i + 1] - row_start[i] tokens of sequence i, min(lo + s code, 65504) in fp32, rounded once to fp16. */
+int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, void *k, int64_t ldk, void *v, int64_t ldv, int n_rows,
+                  void *stream);
+
+/*
+ * out[n_rows][ldo] = softmax(scale q k^T) v per row and query head over the values held in the cache; query heads [j g, (j + 1) g) share key/value head j,
+ * g = n_q_heads / n_kv_heads (a whole number).  The row of new token j of sequence i sees the prefix and the first
+ * kv_len[i] - (row_start[i + 1] - row_start[i]) + j + 1 tokens of its sequence; a row that sees nothing becomes zeros.
+ * Products of fp16 q and codes are exact and summed in fp32; softmax weights are rounded to fp16 before the product with the value codes, their sums are not;
+ * out is rounded once.  Rows of q that hold infinities or NaNs make their own results NaN and no others.
+ * The cache is cut into equal shares over the SMs on the device, from kv_len.  Repeated calls give the same bits; other kv_len of other sequences change
+ * the order of the fp32 sums only.  out may be q (same stride); any other overlap is ROSAQ_ERR_INVALID_ARG.
+ * Uses workspaces of the context that grow on demand (a first call, or one of more prefix rows, may allocate: make it before a capture), so calls of one
+ * context must not overlap on the GPU.
+ */
+int rosaq_attend(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, const void *q, int64_t ldq, int n_q_heads, float scale,
+                 void *out, int64_t ldo, int n_rows, void *stream);
 
 #ifdef __cplusplus
 }

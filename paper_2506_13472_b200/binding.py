@@ -23,8 +23,10 @@ EXPORTS = [
     "rosaq_weight_import", "rosaq_weight_free", "rosaq_weight_info", "rosaq_rotation_create",
     "rosaq_rotation_free", "rosaq_rotate", "rosaq_linear", "rosaq_linear_multi", "rosaq_linear_static",
     "rosaq_plan_equal_shares", "rosaq_plan_create", "rosaq_plan_run", "rosaq_plan_free", "rosaq_plan_ctas",
-    "rosaq_plan_schedule", "rosaq_set_plan_costs", "rosaq_set_plan_pairs",
+    "rosaq_plan_schedule", "rosaq_set_plan_costs", "rosaq_set_plan_pairs", "rosaq_rope_create", "rosaq_rope_free", "rosaq_rope_apply",
+    "rosaq_kv_page_bytes", "rosaq_kv_locate", "rosaq_kv_write", "rosaq_kv_read", "rosaq_attend",
 ]
+ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 
 
 class RosaqError(RuntimeError):
@@ -41,6 +43,21 @@ class _Rot(C.Structure):
 class _Op(C.Structure):
     _fields_ = [("x", C.c_void_p), ("ldx", C.c_int64), ("x_from", C.c_int32), ("r", C.c_void_p), ("w", C.c_void_p),
                 ("y", C.c_void_p), ("ldy", C.c_int64)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("context", C.c_double), ("magnitude", C.c_float)]
+
+
+class _Kv(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("bits", C.c_int32)]
+
+
+class _KvBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("ld_table", C.c_int32), ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("table", C.c_void_p),
+                ("prefix_table", C.c_void_p), ("prefix_tokens", C.c_int32)]
 
 
 _ARRAYS = [(C.c_void_p * n, C.c_int64 * n) for n in range(5)]   # argument arrays of rosaq_linear_multi
@@ -91,6 +108,17 @@ def lib():
         L.rosaq_set_plan_pairs.argtypes = [C.c_void_p, C.c_int]
         L.rosaq_plan_schedule.argtypes = [C.c_int] + [C.POINTER(C.c_int32)] * 5 + [C.c_int, C.POINTER(C.c_int32),
                                                                                   C.POINTER(C.c_int32), C.c_int]
+        L.rosaq_rope_create.argtypes = [C.c_void_p, C.POINTER(_RopeDesc), C.POINTER(C.c_void_p)]
+        L.rosaq_rope_free.argtypes = [C.c_void_p]
+        L.rosaq_rope_apply.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_int64,
+                                       C.c_void_p]
+        L.rosaq_kv_page_bytes.restype = C.c_int64
+        L.rosaq_kv_page_bytes.argtypes = [C.c_int] * 4
+        L.rosaq_kv_locate.argtypes = [C.POINTER(_Kv), C.POINTER(_KvBatch), C.c_int, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
+        L.rosaq_kv_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p]
+        L.rosaq_kv_read.argtypes = L.rosaq_kv_write.argtypes
+        L.rosaq_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float, C.c_void_p, C.c_int64,
+                                   C.c_int, C.c_void_p]
         _lib = L
     return _lib
 
@@ -172,6 +200,54 @@ def plan_schedule(n_tiles, groups, g_fp16, x_from, n_ctas, copies=None):
     assert total2 == total
     pieces = [dict(zip(PIECE_FIELDS, raw[12 * k:12 * k + 12])) for k in range(total)]
     return list(begin), pieces
+
+
+def kv_page_bytes(n_kv_heads, head_dim, bits, page_tokens):
+    """rosaq_kv_page_bytes (host only), or RosaqError."""
+    n = lib().rosaq_kv_page_bytes(int(n_kv_heads), int(head_dim), int(bits), int(page_tokens))
+    if n < 0:
+        raise RosaqError(n, "rosaq_kv_page_bytes")
+    return n
+
+
+def kv_locate(row_start, kv_len, table, rows, n_pages, n_kv_heads, head_dim, bits=4, page_tokens=64):
+    """rosaq_kv_locate (host only) on lists of numbers: (status, offsets, slots) of `rows` rows."""
+    ints = lambda v: (C.c_int32 * max(len(v), 1))(*v)  # noqa: E731
+    n, flat = len(kv_len), ints([p for row in table for p in row])
+    kv = _Kv(16, n_pages, page_tokens, n_kv_heads, head_dim, bits)
+    start, lens = ints(row_start), ints(kv_len)
+    b = _KvBatch(n, len(table[0]), C.addressof(start), C.addressof(lens), C.addressof(flat), None, 0)
+    offset, slot = (C.c_int64 * max(rows, 1))(), (C.c_int32 * max(rows, 1))()
+    st = lib().rosaq_kv_locate(C.byref(kv), C.byref(b), rows, offset, slot)
+    return st, list(offset)[:rows], list(slot)[:rows]
+
+
+class KvCache:
+    """rosaq_kv: the pages (contiguous uint8 CUDA tensor [n_pages][kv_page_bytes]) of a cache of quantized keys and values; keeps them alive."""
+
+    def __init__(self, pages, n_kv_heads, head_dim, bits=4, page_tokens=64):
+        assert pages.is_cuda and pages.dtype is torch.uint8 and pages.dim() == 2 and pages.is_contiguous()
+        assert pages.shape[1] == kv_page_bytes(n_kv_heads, head_dim, bits, page_tokens)
+        self.pages, self.n_kv_heads, self.head_dim, self.bits, self.page_tokens = pages, n_kv_heads, head_dim, bits, page_tokens
+        self.width, self.device = n_kv_heads * head_dim, pages.get_device()
+        self._s = _Kv(pages.data_ptr(), pages.shape[0], page_tokens, n_kv_heads, head_dim, bits)
+        self._p = C.addressof(self._s)
+
+
+class KvBatch:
+    """rosaq_kv_batch: int32 CUDA tensors row_start [n_seqs + 1], kv_len [n_seqs], table [n_seqs][pages of a sequence] (rows contiguous), read on the
+    device whenever a call with the batch runs; prefix = (int32 CUDA tensor of its pages, number of its tokens) or None.  Keeps them alive."""
+
+    def __init__(self, row_start, kv_len, table, prefix=None):
+        n = kv_len.numel()
+        for t in (row_start, kv_len, table) + (() if prefix is None else (prefix[0],)):
+            assert t.is_cuda and t.dtype is torch.int32 and t.stride(-1) == 1 and t.get_device() == kv_len.get_device()
+        assert row_start.dim() == kv_len.dim() == 1 and row_start.numel() == n + 1 and table.dim() == 2 and table.shape[0] == n
+        assert n == 1 or table.stride(0) >= table.shape[1]
+        self.row_start, self.kv_len, self.table, self.prefix, self.device = row_start, kv_len, table, prefix, kv_len.get_device()
+        self._s = _KvBatch(n, table.shape[1] if n == 1 else table.stride(0), row_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(),
+                           None if prefix is None else prefix[0].data_ptr(), 0 if prefix is None else int(prefix[1]))
+        self._p = C.addressof(self._s)
 
 
 class Context:
@@ -307,6 +383,68 @@ class Context:
         _check(lib().rosaq_plan_create(self._h, int(M), len(ops), arr, C.byref(h)), "rosaq_plan_create")
         return Plan(self, h, keep)
 
+    def rope_create(self, head_dim, rot_dim=None, interleaved=False, base=10000.0, scaling="plain", factor=1.0, low=1.0, high=32.0,
+                    context=0.0, magnitude=1.0):
+        """rosaq_rope_create; scaling: a key of ROPE_SCALING."""
+        d = _RopeDesc(head_dim, head_dim if rot_dim is None else rot_dim, 1 if interleaved else 0, ROPE_SCALING[scaling], base, factor, low,
+                      high, context, magnitude)
+        h = C.c_void_p()
+        _check(lib().rosaq_rope_create(self._h, C.byref(d), C.byref(h)), "rosaq_rope_create")
+        return Rope(h, head_dim)
+
+    def rope(self, x, positions, rope, out=None, stream=None):
+        """rosaq_rope_apply on all heads of x's columns; out=x turns them in place."""
+        n, ldx = _act(x)
+        assert positions.is_cuda and positions.dtype is torch.int32 and positions.dim() == 1 and positions.shape[0] == n
+        assert n < 2 or positions.stride(0) == 1
+        heads, rest = divmod(x.shape[1], rope.head_dim)
+        assert rest == 0 and x.get_device() == positions.get_device() == self.device
+        if out is None:
+            out = x.new_empty(x.shape)
+        assert out.shape == x.shape and out.dtype is torch.float16 and out.stride(1) == 1 and out.get_device() == self.device
+        st = lib().rosaq_rope_apply(self._h, rope._h, x.data_ptr(), n, ldx, heads, positions.data_ptr(), out.data_ptr(), out.stride(0),
+                                    _stream(stream, self.device))
+        if st:
+            raise RosaqError(st, "rosaq_rope_apply")
+        return out
+
+    def kv_write(self, cache, batch, k, v, stream=None):
+        """rosaq_kv_write: k, v [rows][n_kv_heads * head_dim]."""
+        (n, ldk), (nv, ldv) = _act(k), _act(v)
+        assert n == nv and k.shape[1] == v.shape[1] == cache.width
+        assert k.get_device() == v.get_device() == cache.device == batch.device == self.device
+        st = lib().rosaq_kv_write(self._h, cache._p, batch._p, k.data_ptr(), ldk, v.data_ptr(), ldv, n, _stream(stream, self.device))
+        if st:
+            raise RosaqError(st, "rosaq_kv_write")
+
+    def kv_read(self, cache, batch, rows, k=None, v=None, stream=None):
+        """rosaq_kv_read into k, v [rows][n_kv_heads * head_dim] (made here if None)."""
+        if k is None:
+            k = torch.empty((rows, cache.width), dtype=torch.float16, device=cache.pages.device)
+        if v is None:
+            v = k.new_empty((rows, cache.width))
+        (n, ldk), (nv, ldv) = _act(k), _act(v)
+        assert n == nv == rows and k.shape[1] == v.shape[1] == cache.width
+        assert k.get_device() == v.get_device() == cache.device == batch.device == self.device
+        st = lib().rosaq_kv_read(self._h, cache._p, batch._p, k.data_ptr(), ldk, v.data_ptr(), ldv, n, _stream(stream, self.device))
+        if st:
+            raise RosaqError(st, "rosaq_kv_read")
+        return k, v
+
+    def attend(self, q, cache, batch, scale=None, out=None, stream=None):
+        """rosaq_attend: q [rows][n_q_heads * head_dim]; scale: head_dim ** -0.5 by default; out=q overwrites the queries."""
+        n, ldq = _act(q)
+        heads, rest = divmod(q.shape[1], cache.head_dim)
+        assert rest == 0 and q.get_device() == cache.device == batch.device == self.device
+        if out is None:
+            out = q.new_empty(q.shape)
+        assert out.shape == q.shape and out.dtype is torch.float16 and out.stride(1) == 1 and out.get_device() == self.device
+        st = lib().rosaq_attend(self._h, cache._p, batch._p, q.data_ptr(), ldq, heads, cache.head_dim ** -0.5 if scale is None else scale,
+                                out.data_ptr(), out.stride(0), n, _stream(stream, self.device))
+        if st:
+            raise RosaqError(st, "rosaq_attend")
+        return out
+
     def linear_static(self, x, weight, rotation=None, out=None, stream=None):
         """rosaq_linear_static: same result as `linear`, but the library allocates nothing (the rotated
         activations live in a fixed 4 MiB array inside the library).  Pass `out`: with out=None this
@@ -388,6 +526,24 @@ class Rotation:
     def free(self):
         if self._h:
             lib().rosaq_rotation_free(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+class Rope:
+    """rosaq_rope wrapper."""
+
+    def __init__(self, handle, head_dim):
+        self._h, self.head_dim = handle, head_dim
+
+    def free(self):
+        if self._h:
+            lib().rosaq_rope_free(self._h)
             self._h = None
 
     def __del__(self):

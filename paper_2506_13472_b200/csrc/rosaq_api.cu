@@ -253,6 +253,10 @@ int rosaq_create(rosaq_ctx **out, int device) {
   ctx->sm_turn = 0;
   for (int i = 0; i < 4; ++i) ctx->pf_clusters[i] = 0;
   ctx->pf_flags = nullptr;
+  ctx->at_partials = ctx->at_prefix = nullptr;
+  ctx->at_partial_bytes = ctx->at_prefix_bytes = 0;
+  ctx->at_arrived = nullptr;
+  for (int &n : ctx->at_per_sm) n = 0;
   ctx->pool = nullptr;
   st = pool_create(ctx);
   if (st == ROSAQ_OK) st = cuda_status(cudaMalloc(reinterpret_cast<void **>(&ctx->d_status), 2 * sizeof(int)));   // [1]: scratch flag of argument checks
@@ -269,6 +273,8 @@ int rosaq_create(rosaq_ctx **out, int device) {
   if (st == ROSAQ_OK) st = cuda_status(cudaMemset(ctx->pl_sync, 0, rosaq::kPlSyncWords * sizeof(unsigned)));
   if (st == ROSAQ_OK) st = cuda_status(cudaMalloc(reinterpret_cast<void **>(&ctx->pf_flags), (size_t)rosaq::kPfFlagsPerSm * ctx->sm_count * sizeof(unsigned)));
   if (st == ROSAQ_OK) st = cuda_status(cudaMemset(ctx->pf_flags, 0, (size_t)rosaq::kPfFlagsPerSm * ctx->sm_count * sizeof(unsigned)));
+  if (st == ROSAQ_OK) st = cuda_status(cudaMalloc(reinterpret_cast<void **>(&ctx->at_arrived), rosaq::kAtMaxCtas * sizeof(int)));
+  if (st == ROSAQ_OK) st = cuda_status(cudaMemset(ctx->at_arrived, 0, rosaq::kAtMaxCtas * sizeof(int)));
   // the partial tiles of a launch whose CTAs all share tiles at both ends of two phases (grown if a plan needs more), and of one on the
   // prefill tiles
   const size_t tile_bytes = (size_t)4 * ctx->sk_ctas * rosaq::kSkPartialBytes;
@@ -280,6 +286,7 @@ int rosaq_create(rosaq_ctx **out, int device) {
     if (ctx->pl_sync) (void)cudaFree(ctx->pl_sync);
     if (ctx->sm_between) (void)cudaFree(ctx->sm_between);
     if (ctx->pf_flags) (void)cudaFree(ctx->pf_flags);
+    if (ctx->at_arrived) (void)cudaFree(ctx->at_arrived);
     if (ctx->pl_exchange) (void)cudaFree(ctx->pl_exchange);
     if (ctx->pf_partials) (void)cudaFree(ctx->pf_partials);
     if (ctx->d_status) (void)cudaFree(ctx->d_status);
@@ -306,8 +313,11 @@ int rosaq_destroy(rosaq_ctx *ctx) {
     if (ctx->pl_sync) (void)cudaFree(ctx->pl_sync);
     if (ctx->sm_between) (void)cudaFree(ctx->sm_between);
     if (ctx->pf_flags) (void)cudaFree(ctx->pf_flags);
+    if (ctx->at_arrived) (void)cudaFree(ctx->at_arrived);
     if (ctx->pl_exchange) (void)cudaFree(ctx->pl_exchange);
     if (ctx->pf_partials) (void)cudaFree(ctx->pf_partials);
+    if (ctx->at_partials) (void)cudaFree(ctx->at_partials);
+    if (ctx->at_prefix) (void)cudaFree(ctx->at_prefix);
     plan_free_schedules(ctx);
     pool_release(ctx->pool);
     (void)cudaGetLastError();
@@ -698,16 +708,8 @@ int rosaq_plan_create(rosaq_ctx *ctx, int M, int n_ops, const rosaq_op *ops, ros
   }
   // an output may be read only through x_from (which orders the two operations) and written by one
   // operation: any other overlap of a y with an x or a y would be a race inside the launch
-  // (views of M rows: with equal row strides, disjoint column ranges of one wider buffer do not overlap)
   auto overlap = [M](const void *pa, int64_t lda, int da, const void *pb, int64_t ldb, int db) {
-    const char *alo = static_cast<const char *>(pa), *blo = static_cast<const char *>(pb);
-    const char *ahi = alo + sizeof(__half) * ((size_t)(M - 1) * (size_t)lda + (size_t)da);
-    const char *bhi = blo + sizeof(__half) * ((size_t)(M - 1) * (size_t)ldb + (size_t)db);
-    if (!(alo < bhi && blo < ahi)) return false;
-    if (lda != ldb) return true;
-    const long long off = (blo - alo) / (long long)sizeof(__half);
-    const long long c = ((off % lda) + lda) % lda;              // b's first column inside a's rows
-    return !(c >= da && c + db <= lda);
+    return views_overlap(M, pa, lda, da, pb, ldb, db);
   };
   for (int i = 0; i < n_ops && st == ROSAQ_OK; ++i) {
     const PlanOp &a = pl->ops[i];

@@ -251,6 +251,7 @@ struct MemPool {
 
 namespace rosaq {
 constexpr int kMaxRetired = 96;
+constexpr int kAtMaxCtas = 2048;                    // attention over the cache: CTAs of a launch
 }
 
 struct rosaq_ctx {
@@ -285,6 +286,13 @@ struct rosaq_ctx {
   float *pf_partials;                            // partial tiles of a launch cut into equal shares
   size_t pf_partial_bytes;
   int pf_clusters[4];                            // clusters of 1 .. 4 pairs the device keeps resident at once (0 until first asked for)
+  // attention over the cache (attend.cu)
+  float *at_partials;                            // partial tiles of query rows, grown on demand
+  size_t at_partial_bytes;
+  float *at_prefix;                              // what a batch found in its shared prefix, grown on demand
+  size_t at_prefix_bytes;
+  int *at_arrived;                               // [kAtMaxCtas] CTAs that have stored their partial tile; zero between launches
+  int at_per_sm[12];                             // resident CTAs per SM of each variant (0 until first asked for)
   unsigned *pf_flags;                            // [pair][2][rank]: readers that have yet to fetch a partial tile; zero between launches
 };
 
@@ -384,6 +392,18 @@ inline int grow_exchange(rosaq_ctx *ctx, size_t need) {
   (void)cudaGetLastError();
   ctx->pl_exchange_bytes = 0;   // (not to be used as it is: the next call grows it again)
   return ROSAQ_ERR_CUDA;
+}
+
+// Whether two views of `rows` rows of fp16 share an element (with equal row strides, disjoint column ranges of one wider buffer do not).
+inline bool views_overlap(int rows, const void *pa, int64_t lda, int64_t da, const void *pb, int64_t ldb, int64_t db) {
+  const char *alo = static_cast<const char *>(pa), *blo = static_cast<const char *>(pb);
+  const char *ahi = alo + sizeof(__half) * ((size_t)(rows - 1) * (size_t)lda + (size_t)da);
+  const char *bhi = blo + sizeof(__half) * ((size_t)(rows - 1) * (size_t)ldb + (size_t)db);
+  if (!(alo < bhi && blo < ahi)) return false;
+  if (lda != ldb) return true;
+  const long long off = (blo - alo) / (long long)sizeof(__half);
+  const long long c = ((off % lda) + lda) % lda;              // b's first column inside a's rows
+  return !(c >= da && c + db <= lda);
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
