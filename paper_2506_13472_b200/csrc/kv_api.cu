@@ -192,6 +192,7 @@ int rosaq_attend(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch
   if (batch->prefix_tokens < 0 || (batch->prefix_tokens > 0 && !batch->prefix_table)) return ROSAQ_ERR_INVALID_ARG;
   if (batch->prefix_tokens > 1 << 30) return ROSAQ_ERR_UNSUPPORTED_SHAPE;
   if (batch->prefix_tokens > 0 && (reinterpret_cast<uintptr_t>(batch->prefix_table) & 3)) return ROSAQ_ERR_ALIGNMENT;
+  if ((int64_t)n_rows * n_q_heads > (int64_t)1 << 30) return ROSAQ_ERR_UNSUPPORTED_SHAPE;
   st = check_rows(q, n_rows, ldq, d);
   if (st == ROSAQ_OK) st = check_rows(out, n_rows, ldo, d);
   if (st != ROSAQ_OK || n_rows == 0) return st;
