@@ -89,6 +89,7 @@ __device__ __forceinline__ Seq load_seq(const AtParams &p, int i, bool report) {
   return s;
 }
 
+__device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -161,14 +162,13 @@ struct Cfg {
   static constexpr bool kQShared = kTiles > 2 || (kTiles == 1 && QS1);      // B fragments of the queries in shared memory rather than in registers, each warp its own
   static constexpr int kQBytes = kQShared ? kWarps * kTiles * kHd / 16 * 256 : 0;
   static constexpr int kPairBytes = kChunk * kKvBlock * 20;   // of a warp: what its tokens' pairs become
-  static constexpr int kRoom = 222 * 1024 / kPerSm - kQBytes - 1024 - (kPairBytes + 48 + 64) * kWarps;
+  static constexpr int kRoom = 222 * 1024 / kPerSm - kQBytes - 1024 - (kPairBytes + 64 + 64) * kWarps;
   static constexpr int kDepth = kRoom / kStageBytes / kWarps < 32 / kWarps ? kRoom / kStageBytes / kWarps : 32 / kWarps;   // slots of a warp, next to each other
   static constexpr int kStages = kWarps * kDepth;
-  static constexpr int kSmem = kStages * kStageBytes + kQBytes + kPairBytes * kWarps + 16 * kStages + 48 * kWarps + 64;
+  static constexpr int kSmem = kStages * kStageBytes + kQBytes + kPairBytes * kWarps + 16 * kStages + 64 * kWarps + 64;
   static constexpr bool kSlotsHold = kDepth * kStageBytes >= kFragBytes;   // a part of a tile
   static constexpr int kPartial = kRows * (kHd + 4);   // floats of a partial tile: [row][kHd], then [row]{maximum, sum}, padded
   static constexpr long long kWorkBytes = 2 * 4 * kPartial + 2 * kWarps * kFragBytes;   // of a CTA: partial tiles, parts that the slots do not hold
-  static constexpr int kLeast = kWarps;             // chunks that make a CTA of its own worth while
   static_assert(kChunk == 2 && kDepth >= 1 && kStages <= 32, "slots");
 };
 
@@ -194,11 +194,42 @@ __device__ __forceinline__ bool settle(const AtParams &p, Cursor &c) {
   return true;
 }
 
+// How the list is cut.  Even shares, except that
+//   - tiles of few chunks are not cut where there is no need: joining the parts of several CTAs takes about 5 us, a warp's chunk 0.8 (one sequence of 333 tokens,
+//     32 heads: 13.8 us in 50 shares of seven chunks, .. in 32 shares of a tile), and
+//   - a cut that would fall within `near` chunks of the end of a tile moves there.
+// Divisions are 32-bit ones wherever the numbers are small: a 64-bit one takes a lone warp 0.2 us.
+__device__ __forceinline__ long long divide(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
+struct Shares {
+  long long total, part;                            // part = total / ctas, and what is left
+  int ctas, left, near;
+  __device__ __forceinline__ long long even(int c) const { return part * c + (uint32_t)(left * c) / (uint32_t)ctas; }
+  // the last CTA whose even share begins at or before `at`
+  __device__ __forceinline__ int owner(long long at) const {
+    int c = min(max((int)((float)at * (float)ctas / (float)total), 0), ctas - 1);   // within one of it
+    while (even(c) > at) --c;
+    while (c + 1 < ctas && even(c + 1) <= at) ++c;
+    return c;
+  }
+  __device__ __forceinline__ int snap(int chunk, int chunks) const { return chunk <= near ? -chunk : chunks - chunk <= near ? chunks - chunk : 0; }
+  // the CTAs that hold chunks of the tile [at, at + chunks)
+  __device__ __forceinline__ int first(long long at, int chunks) const { return owner(at + min(near, chunks - 1)); }
+  __device__ __forceinline__ int last(long long at, int chunks) const { return max(first(at, chunks), owner(at + max(chunks - 1 - near, 0))); }
+};
+__device__ __forceinline__ Shares make_shares(long long total, int units, int warps, int tiles, int most) {
+  Shares s;
+  s.total = total;
+  s.ctas = (int)min((long long)most, total < 8ll * warps * units ? (long long)units : divide(total, warps));
+  s.part = divide(total, s.ctas), s.left = (int)(total - s.part * s.ctas);
+  s.near = (int)min(8ll / tiles, s.part / 8);
+  return s;
+}
+
 // A part of a tile, as its warp leaves it.
 struct Frag {
   int from;             // first chunk of the tile, counted from the CTA's first; kNoFrag: none
   int seq, unit, chunks;
-  int in_slots;
+  const float *data;
 };
 constexpr int kNoFrag = INT_MIN;
 
@@ -256,10 +287,9 @@ attend_kernel(const __grid_constant__ AtParams p) {
   float4 *const pair_terms = reinterpret_cast<float4 *>(q_frags + C::kQBytes / 8);        // [warp][token]{s_k', lo_k, log2 s_v, 1 / s_v}, [token] lo_v / s_v + middle
   uint64_t *const bars = reinterpret_cast<uint64_t *>(pair_terms + C::kPairBytes / 16 * kWarps);
   Frag *const frags = reinterpret_cast<Frag *>(bars + 2 * C::kStages);                    // [warp]{first part of a tile that began before, last one}
-  int *const flag = reinterpret_cast<int *>(frags + 2 * kWarps);                          // [2]
+  int *const flag = reinterpret_cast<int *>(frags + 2 * kWarps);                          // [2]{first, last CTA} of tiles that other CTAs hold parts of
   // Parts of tiles: a warp's last one lies in its slots, where they are large enough, an earlier one behind the partial tiles of all CTAs.
   uint8_t *const parts = reinterpret_cast<uint8_t *>(p.partials + 2ll * gridDim.x * C::kPartial) + (long long)blockIdx.x * 2 * kWarps * C::kFragBytes;
-  auto part_of = [&](int w, int which, int in_slots) { return in_slots ? ring + w * C::kDepth * C::kStageBytes : parts + (2 * w + which) * C::kFragBytes; };
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
 
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::kStages;
@@ -274,17 +304,24 @@ attend_kernel(const __grid_constant__ AtParams p) {
 
   // ---- the share of this CTA; every warp works it out
   long long total = 0;
+  int units = 0;
 #pragma unroll 4
-  for (int i = lane; i < p.b.n_seqs; i += 32) total += load_seq<kRows>(p, i, blockIdx.x == 0 && warp == 0).cost;
+  for (int i = lane; i < p.b.n_seqs; i += 32) {
+    const Seq s = load_seq<kRows>(p, i, blockIdx.x == 0 && warp == 0);
+    total += s.cost, units += s.tiles;
+  }
 #pragma unroll
-  for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
-  const int ctas = (int)max(1ll, min((long long)gridDim.x, total / C::kLeast)), cta = blockIdx.x;
-  if (cta >= ctas || total == 0) return;
-  const long long begin = total * cta / ctas, end = total * (cta + 1) / ctas;
-  const int n = (int)(end - begin);                 // chunks of this CTA (a share of 2^31 would be 4 TB of cache)
+  for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d), units += __shfl_xor_sync(0xffffffffu, units, d);
+  units *= p.kv.n_heads;
+  if (total == 0) return;
+  const Shares shares = make_shares(total, units, kWarps, kTiles, gridDim.x);
+  const int ctas = shares.ctas, cta = blockIdx.x;
+  if (cta >= ctas) return;
+  long long begin, end;
   Cursor cur;
   {
-    // the sequence that holds `begin`
+    // the sequence that holds the first chunk of an even share
+    const long long even = shares.even(cta);
     long long base = 0;
     cur.seq = 0;
     for (int i = 0; i < p.b.n_seqs; i += 32) {
@@ -295,7 +332,7 @@ attend_kernel(const __grid_constant__ AtParams p) {
         const long long o = __shfl_up_sync(0xffffffffu, sum, d);
         if (lane >= d) sum += o;
       }
-      const unsigned past = __ballot_sync(0xffffffffu, base + sum > begin);
+      const unsigned past = __ballot_sync(0xffffffffu, base + sum > even);
       if (past) {
         const int k = __ffs(past) - 1;
         cur.seq = i + k;
@@ -305,10 +342,22 @@ attend_kernel(const __grid_constant__ AtParams p) {
       base += __shfl_sync(0xffffffffu, sum, 31);
     }
     cur.s = load_seq<kRows>(p, cur.seq, false);
-    cur.unit = (int)((begin - base) / cur.s.chunks), cur.chunk = (int)((begin - base) - (long long)cur.unit * cur.s.chunks);
+    cur.unit = (int)divide(even - base, cur.s.chunks), cur.chunk = (int)((even - base) - (long long)cur.unit * cur.s.chunks);
+    const int moved = shares.snap(cur.chunk, cur.s.chunks);
+    begin = even + moved, cur.chunk += moved;        // (perhaps behind the tile's last chunk: settled below)
+    // and where the next CTA's begins, by the same rule
+    end = total;
+    if (cta + 1 < ctas) {
+      const long long next = shares.even(cta + 1);
+      Cursor c = cur;
+      c.chunk += (int)(next - begin);
+      settle<kRows>(p, c);
+      end = next + shares.snap(c.chunk, c.s.chunks);
+    }
   }
-  // warp w takes chunks [n w / kWarps, n (w + 1) / kWarps) of the CTA's: long runs, so that a warp seldom changes its tile and never waits for another
-  auto bound = [&](int w) { return (int)((long long)n * w / kWarps); };
+  const int n = (int)(end - begin);                 // chunks of this CTA (a share of 2^31 would be 4 TB of cache)
+  // warp w takes chunks [n w / kWarps, n (w + 1) / kWarps), rounded up (warp 0 always has one), of the CTA's: long runs, so that a warp seldom changes its tile and never waits for another
+  auto bound = [&](int w) { return (int)(((long long)n * w + kWarps - 1) / kWarps); };
 
   if (warp == kWarps) {
     // ---- producer: lane i fills slot i, with chunks i % kDepth, i % kDepth + kDepth, ... of warp i / kDepth.  The lanes go round together and none waits for
@@ -627,8 +676,9 @@ attend_kernel(const __grid_constant__ AtParams p) {
 
     // ---- the tile's rows, or this warp's part of them
     const bool whole = chunk0 == 0 && j1 - j0 == s.chunks;
-    const int which = chunk0 != 0 ? 0 : 1, in_slots = C::kSlotsHold && j == last;   // (no chunk is left: the slots are free)
-    float *const part = reinterpret_cast<float *>(part_of(warp, which, in_slots));
+    const int which = chunk0 != 0 ? 0 : 1;
+    // (no chunk left: the slots are free)
+    float *const part = reinterpret_cast<float *>(C::kSlotsHold && j == last ? ring + warp * C::kDepth * C::kStageBytes : parts + (2 * warp + which) * C::kFragBytes);
 #pragma unroll
     for (int i = 0; i < 2 * kTiles; ++i) {
       const int t = i >> 1, e = i & 1, row = 8 * t + 2 * c + e;
@@ -672,38 +722,52 @@ attend_kernel(const __grid_constant__ AtParams p) {
         }
       }
     }
-    if (!whole && lane == 0) frags[2 * warp + which] = Frag{j0 - chunk0, cur.seq, cur.unit, s.chunks, in_slots};
+    if (!whole && lane == 0) frags[2 * warp + which] = Frag{j0 - chunk0, cur.seq, cur.unit, s.chunks, part};
   }
 
-  // ---- tiles that several warps hold parts of: a chain of the last part of one warp (or the first one of warp 0, when the CTA's share begins inside a tile) and the first
+  // ---- tiles that several warps hold parts of: chains of the last part of one warp (or the first one of warp 0, when the CTA's share begins inside a tile) and the first
   // parts of those behind it
   asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory");
-  int open[2] = {-1, -1};                            // chains of tiles that other CTAs hold parts of too: entered from, or left to, them
+  // One warp per chain, or all on the only one and on those of large tiles.
+  int chains = 0;
 #pragma unroll 1
-  for (int lead = -1; lead < kWarps; ++lead) {
+  for (int lead = -1; lead < kWarps; ++lead) chains += frags[lead < 0 ? 0 : 2 * lead + 1].from != kNoFrag;
+  const bool alone = kTiles == 1 && chains > 1;
+  int open = -1;                                     // the chain that is left to other CTAs, if it begins here
+#pragma unroll 1
+  for (int lead = -1, k = 0; lead < kWarps; ++lead) {
     const Frag f = frags[lead < 0 ? 0 : 2 * lead + 1];
     if (f.from == kNoFrag) continue;
+    const bool whole = f.from >= 0 && f.from + f.chunks <= n;
+    if (!whole && lead >= 0) open = lead;
+    if (alone && k++ % kWarps != warp) continue;
     const Seq s = load_seq<kRows>(p, f.seq, false);
     const int head = f.unit / s.tiles, first_row = (f.unit - head * s.tiles) * kRows, rows = min(kRows, s.rows * p.group - first_row);
-    unsigned members = 0;                            // warps whose first part belongs to it
-    for (int w = lead < 0 ? 0 : lead + 1; w < kWarps; ++w)
-      if (frags[2 * w].from == f.from) members |= 1u << w;
-    const bool whole = f.from >= 0 && f.from + f.chunks <= n;
-    if (!whole) open[f.from < 0 ? 0 : 1] = lead;
+    const float *member[kWarps];                     // the parts that belong to it
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const Frag &g = frags[2 * w + (w == lead)];
+      member[w] = w >= lead && g.from == f.from ? g.data : nullptr;
+    }
     float *const to = p.partials + (long long)(2 * cta + (f.from < 0 ? 0 : 1)) * C::kPartial;
-    for (int i = threadIdx.x; i < rows * (kHd / 4); i += kConsumers) {
+#pragma unroll 1
+    for (int i = alone ? lane : threadIdx.x; i < rows * (kHd / 4); i += alone ? 32 : kConsumers) {
       const int row = i / (kHd / 4), ch = 4 * (i % (kHd / 4));
       float m = kNone, l = 0.f;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto add = [&](int w, int which) {
-        const float *const x = reinterpret_cast<const float *>(part_of(w, which, frags[2 * w + which].in_slots));
-        const float4 u = reinterpret_cast<const float4 *>(x + kRows * C::kAccLd)[row];
-        float4 v = *reinterpret_cast<const float4 *>(x + row * C::kAccLd + ch);
-        v.x += u.z, v.y += u.z, v.z += u.z, v.w += u.z;
-        join(a, m, l, v, u.x, u.y);
-      };
-      if (lead >= 0) add(lead, 1);
-      for (unsigned w = members; w; w &= w - 1) add(__ffs(w) - 1, 0);
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), u[kWarps];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        u[w] = member[w] ? reinterpret_cast<const float4 *>(member[w] + kRows * C::kAccLd)[row] : make_float4(kNone, 0.f, 0.f, 0.f);
+        m = fmaxf(m, u[w].x);
+      }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        if (!member[w]) continue;
+        const float4 v = *reinterpret_cast<const float4 *>(member[w] + row * C::kAccLd + ch);
+        const float g = ex2(u[w].x - m);
+        a.x = __fmaf_rn(g, v.x + u[w].z, a.x), a.y = __fmaf_rn(g, v.y + u[w].z, a.y), a.z = __fmaf_rn(g, v.z + u[w].z, a.z), a.w = __fmaf_rn(g, v.w + u[w].z, a.w);
+        l = __fmaf_rn(g, u[w].y, l);
+      }
       if (whole) {
         store_row4<kHd>(p, row_at<kHd>(p, s.row, head, first_row + row), ch, a, m, l);
       } else {
@@ -712,59 +776,63 @@ attend_kernel(const __grid_constant__ AtParams p) {
       }
     }
   }
-  // (a tile that covers the CTA's whole share and more is in open[0] or, when it begins here, in open[1])
-  const bool enters = frags[0].from != kNoFrag && frags[0].from < 0;
-  if (open[0] < 0 && !enters && open[1] < 0) return;
-  __threadfence();
+  // ---- tiles that other CTAs hold parts of too: one that began before this share, one that is left to the next ones
+  const bool enters = frags[0].from != kNoFrag;
+  if (!enters && open < 0) return;
+  const int mine = warp == 0 && enters ? 0 : warp == 1 && open >= 0 ? 2 * open + 1 : -1;   // warp 0 sees to the one, warp 1 to the other
+  int *const span = flag + 2 * warp;                 // [2][first, last]
+  if (mine >= 0 && lane == 0) span[0] = shares.first(begin + frags[mine].from, frags[mine].chunks), span[1] = shares.last(begin + frags[mine].from, frags[mine].chunks);
   asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory");
-  int c0[2], c1[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const Frag f = frags[i == 0 ? 0 : max(2 * open[1] + 1, 0)];
-    // the CTAs that hold chunks [first, first + f.chunks) of the list
-    const long long first = begin + f.from;
-    const bool is = i == 0 ? enters : open[1] >= 0;
-    c0[i] = c1[i] = -1;
-    if (!is) continue;
-    c0[i] = (int)(((first + 1) * ctas + total - 1) / total) - 1, c1[i] = (int)(((first + f.chunks) * ctas + total - 1) / total) - 1;
-    if (threadIdx.x == 0) {
-      const bool all = atomicAdd(p.arrived + c0[i], 1) == c1[i] - c0[i];
-      if (all) p.arrived[c0[i]] = 0;
-      flag[i] = all;
-    }
+  if (mine >= 0 && lane == 0) {
+    // (cumulative: what the barrier has made this thread see is visible to whoever sees the count, and the other way round)
+    fence_gpu();
+    const bool all = atomicAdd(p.arrived + span[0], 1) == span[1] - span[0];
+    fence_gpu();
+    if (all) p.arrived[span[0]] = 0;
+    else span[0] = -1;
   }
   asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory");
   float4 *const scratch = reinterpret_cast<float4 *>(ring);   // (nothing in the slots is needed any more)
 #pragma unroll 1
   for (int o = 0; o < 2; ++o) {
-    if (c0[o] < 0 || !flag[o]) continue;
+    const int c0 = flag[2 * o], c1 = flag[2 * o + 1];
+    if ((o == 0 ? !enters : open < 0) || c0 < 0) continue;
     // ---- this CTA is the last one: the partial tiles of all, in the order of the list
-    __threadfence();
-    const Frag f = frags[o == 0 ? 0 : 2 * open[1] + 1];
+    const Frag f = frags[o == 0 ? 0 : 2 * open + 1];
     const Seq s = load_seq<kRows>(p, f.seq, false);
     const int head = f.unit / s.tiles, first_row = (f.unit - head * s.tiles) * kRows, rows = min(kRows, s.rows * p.group - first_row);
     // an item is four channels of a row; where there are fewer than threads, several threads take every `split`-th partial tile each
     const int items = rows * (kHd / 4), split = max(1, kConsumers / items);
+#pragma unroll 1
     for (int i = threadIdx.x; i < items * split; i += kConsumers) {
       const int item = i % items, row = item / (kHd / 4), ch = 4 * (item % (kHd / 4));
       float m = kNone, l = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
       constexpr int kAhead = 8;                      // loads in flight
-      for (int k = c0[o] + i / items; k <= c1[o]; k += kAhead * split) {
+      for (int k = c0 + i / items; k <= c1; k += kAhead * split) {
         float4 x[kAhead];
         float2 ml[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
           const int kk = k + u * split;
-          const float *const from = p.partials + (long long)(2 * kk + (kk == c0[o])) * C::kPartial;
+          const float *const from = p.partials + (long long)(2 * kk + (kk == c0)) * C::kPartial;
           ml[u] = make_float2(kNone, 0.f), x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (kk <= c1[o]) {
+          if (kk <= c1) {
             x[u] = __ldcg(reinterpret_cast<const float4 *>(from + row * kHd + ch));
             ml[u] = __ldcg(reinterpret_cast<const float2 *>(from + kRows * kHd + 2 * row));
           }
         }
+        float mm = m;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) join(a, m, l, x[u], ml[u].x, ml[u].y);
+        for (int u = 0; u < kAhead; ++u) mm = fmaxf(mm, ml[u].x);
+        float f = ex2(m - mm);
+        a = make_float4(a.x * f, a.y * f, a.z * f, a.w * f), l *= f, m = mm;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          f = ex2(ml[u].x - m);
+          a.x = __fmaf_rn(x[u].x, f, a.x), a.y = __fmaf_rn(x[u].y, f, a.y), a.z = __fmaf_rn(x[u].z, f, a.z), a.w = __fmaf_rn(x[u].w, f, a.w);
+          l = __fmaf_rn(ml[u].y, f, l);
+        }
       }
       if (split == 1) store_row4<kHd>(p, row_at<kHd>(p, s.row, head, first_row + row), ch, a, m, l);
       else scratch[2 * i] = a, scratch[2 * i + 1] = make_float4(m, l, 0.f, 0.f);
