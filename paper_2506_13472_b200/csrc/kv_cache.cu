@@ -5,20 +5,25 @@
 // lies on one side of zero loses no range (the weights' integer zero-point would).
 //
 // Bound: memory (rows in, 0.27 or 0.52 of their bytes out).  One warp takes one block of 16 tokens of one head, keys or values: rows
-// arrive as 16 bytes per lane (a row is contiguous over 16 or 8 lanes), codes go through 4 KB of shared memory as 16-bit numbers, and
+// arrive as 16 bytes per lane in 4 KB of shared memory (a row is contiguous over 16 or 8 lanes), codes take their place as 16-bit numbers, and
 // ldmatrix hands every lane the pairs whose nibbles or bytes make up its words: plain for keys, transposed for values.  Whole
-// blocks leave as 16-byte stores; the bytes of a block that begins or ends inside it are stored one by one.
+// blocks leave as 16-byte stores; into those that begin or end inside a block the bytes of the other tokens are read first (bytes stored one by one would be 190 partial
+// sectors per token and head, 64 x 32 of them 6.9 us).  One warp of a call writes to a block, so nothing comes between.
 #include "kv_common.cuh"
 
 namespace rosaq {
 namespace {
 
-constexpr int kWarps = 8;                           // four heads, keys and values
+constexpr int kWarps = 4;                           // two heads, keys and values
 constexpr int kHeadsPerCta = kWarps / 2;
 
 __device__ __forceinline__ uint32_t h2_bits(__half2 v) { return *reinterpret_cast<uint32_t *>(&v); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t v) { return *reinterpret_cast<__half2 *>(&v); }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t *a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
@@ -43,104 +48,128 @@ __device__ __forceinline__ void stmatrix4_trans(uint32_t addr, const uint32_t *a
 // Shared address of the row that this lane names to ldmatrix / stmatrix for channels [16 j, 16 j + 16) of 16 tokens.  The four 8 x 8
 // matrices are the A fragment's: keys (tokens 0-7, channels 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15); values, whose rows are
 // channels, the same with the parts of tokens and channels exchanged.
-template <bool kValue>
-__device__ __forceinline__ uint32_t frag_addr(uint32_t tile, int row_bytes, int lane, int j) {
+__device__ __forceinline__ uint32_t frag_addr(uint32_t tile, int row_bytes, int lane, int j, bool value) {
   const int a = (lane >> 3) & 1, b = lane >> 4;
-  const int tok = (lane & 7) + 8 * (kValue ? b : a), ch = 16 * j + 8 * (kValue ? a : b);
+  const int tok = (lane & 7) + 8 * (value ? b : a), ch = 16 * j + 8 * (value ? a : b);
   return tile + tok * row_bytes + 2 * ch;
 }
 
-template <int kHd, int kBits, bool kValue>
-__device__ __forceinline__ void write_block(const KvPiece &p, const __half *x, long long ldx, uint8_t *block, uint32_t tile) {
+// (least, minus the greatest) of eight values; kSkip: of those that are numbers, else a NaN where one is
+template <bool kSkip>
+__device__ __forceinline__ __half2 range(const uint32_t *w) {
+  const __half2 a = bits_h2(w[0]), b = bits_h2(w[1]), c = bits_h2(w[2]), d = bits_h2(w[3]);
+  const __half2 lo = kSkip ? __hmin2(__hmin2(a, b), __hmin2(c, d)) : __hmin2_nan(__hmin2_nan(a, b), __hmin2_nan(c, d));
+  const __half2 hi = kSkip ? __hmax2(__hmax2(a, b), __hmax2(c, d)) : __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d));
+  const __half l = kSkip ? __hmin(__low2half(lo), __high2half(lo)) : __hmin_nan(__low2half(lo), __high2half(lo));
+  const __half h = kSkip ? __hmax(__low2half(hi), __high2half(hi)) : __hmax_nan(__low2half(hi), __high2half(hi));
+  return __halves2half2(l, __hneg(h));
+}
+
+// Keys and values take the same code (which of them is uniform in a warp) and its loops are rolled: small calls spend more time on fetching instructions than on anything else.
+template <int kHd, int kBits>
+__device__ __forceinline__ void write_block(bool value, const KvPiece &p, const __half *x, long long ldx, uint8_t *block, uint32_t tile) {
   constexpr int kLanes = kHd / 8, kPer = 32 / kLanes, kSteps = kKvBlock / kPer;   // lanes of a token, tokens and loads of a step
   constexpr int kRowBytes = 2 * kHd + 16;                                         // 16 more: rows on different banks
   constexpr int kWords = kHd / 16 * (kBits / 4);
   constexpr float kMax = kBits == 4 ? 15.f : 255.f;
   const int lane = threadIdx.x & 31, part = lane % kLanes, mine = lane / kLanes;
-  uint4 in[kSteps];
+  const uint32_t cell = tile + mine * kRowBytes + 16 * part;   // this lane's 16 bytes of the first step's tokens: values, then 16-bit codes
+  // ---- the rows, as far as shared memory; every lane uses what it has brought itself
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int t = i * kPer + mine - p.slot;
-    in[i] = make_uint4(0, 0, 0, 0);
-    if (t >= 0 && t < p.n) in[i] = __ldg(reinterpret_cast<const uint4 *>(x + (p.row + t) * ldx + 8 * part));
+    if (t >= 0 && t < p.n) copy16(cell + i * kPer * kRowBytes, x + (p.row + t) * ldx + 8 * part);
   }
-  uint8_t *const params = block + 2 * kv_code_bytes(kHd, kBits) + (kValue ? 4 * kKvBlock : 0);
+  uint8_t *const codes = block + (value ? kv_code_bytes(kHd, kBits) : 0) + 16 * lane;
+  // which bytes of this lane's words (even and odd ones) are this piece's, and what is there now
+  uint32_t ours[2] = {0xffffffffu, 0xffffffffu};
+  uint4 old[kWords / 4];
+  if (p.n != kKvBlock) {
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
+    for (int e = 0; e < 2; ++e) {
+      ours[e] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = (value ? kv_byte_token<kBits, true>(lane, e, j) : kv_byte_token<kBits, false>(lane, e, j)) - p.slot;
+        if (t >= 0 && t < p.n) ours[e] |= 0xffu << (8 * j);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kWords / 4; ++q)
+      if (ours[0] | ours[1]) old[q] = *reinterpret_cast<const uint4 *>(codes + 512 * q);
+  }
+  copy_wait_all();
+  uint8_t *const params = block + 2 * kv_code_bytes(kHd, kBits) + (value ? 4 * kKvBlock : 0);
+#pragma unroll 1
+  for (int i = p.slot / kPer; i * kPer < p.slot + p.n; ++i) {
     const int t = i * kPer + mine;
     const bool valid = t >= p.slot && t < p.slot + p.n;
-    if (!__any_sync(0xffffffffu, valid)) continue;
-    const uint32_t w[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
-    // (least, minus the greatest); a NaN is in neither
-    __half2 lo2 = __hmin2(__hmin2(bits_h2(w[0]), bits_h2(w[1])), __hmin2(bits_h2(w[2]), bits_h2(w[3])));
-    __half2 hi2 = __hmax2(__hmax2(bits_h2(w[0]), bits_h2(w[1])), __hmax2(bits_h2(w[2]), bits_h2(w[3])));
-    __half2 m = __halves2half2(__hmin(__low2half(lo2), __high2half(lo2)), __hneg(__hmax(__low2half(hi2), __high2half(hi2))));
+    const uint4 in = valid ? lds128(cell + i * kPer * kRowBytes) : make_uint4(0, 0, 0, 0);
+    uint32_t w[4] = {in.x, in.y, in.z, in.w};
+    // (least, minus the greatest).  Almost always all are numbers: NaNs come through this way, and what is not finite is seen to apart.
+    __half2 m = range<false>(w);
 #pragma unroll
-    for (int d = kLanes / 2; d > 0; d /= 2) m = __hmin2(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), d)));
+    for (int d = kLanes / 2; d > 0; d /= 2) m = __hmin2_nan(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), d)));
     float lo = __low2float(m), hi = -__high2float(m);
-    if (isnan(lo)) lo = hi = 0.f;
-    lo = fminf(fmaxf(lo, -65504.f), 65504.f) + 0.f, hi = fminf(fmaxf(hi, -65504.f), 65504.f);
+    if (__any_sync(0xffffffffu, !(lo >= -65504.f && hi <= 65504.f))) {
+      m = range<true>(w);                            // a NaN is in neither
+#pragma unroll
+      for (int d = kLanes / 2; d > 0; d /= 2) m = __hmin2(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), d)));
+      lo = __low2float(m), hi = -__high2float(m);
+      if (isnan(lo)) lo = hi = 0.f;
+      lo = fminf(fmaxf(lo, -65504.f), 65504.f), hi = fminf(fmaxf(hi, -65504.f), 65504.f);
+      // infinities end up at the ends of the range, a NaN at its least value
+      const __half2 least = __float2half2_rn(lo);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const __half2 c = __hmin2(__hmax2(bits_h2(w[e]), bits_h2(0xfbfffbffu)), bits_h2(0x7bff7bffu));
+        w[e] = h2_bits(__hmax2(c, least));           // (a NaN came out of the two before as -65504)
+      }
+    }
+    lo += 0.f;                                       // (no negative zero)
     __half sh = __float2half_rn(__fdiv_rn(hi - lo, kMax));
     if (__half_as_ushort(sh) == 0) sh = __ushort_as_half(1);
     const float s = __half2float(sh), inv = __frcp_rn(s);
-    uint32_t code[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // infinities end up at the ends of the range, a NaN at its least value
-      const __half2 c = __hmin2(__hmax2(bits_h2(w[e]), bits_h2(0xfbfffbffu)), bits_h2(0x7bff7bffu));
-      const float xs[2] = {__low2float(c), __high2float(c)};
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        // (x - lo) / s rounded correctly from the rounded reciprocal: one residual and one correction (Markstein, "Computation of
-        // elementary functions on the IBM RISC System/6000 processor", 1990).  A product with the reciprocal alone would move the
-        // ties, which fp16 data meets once in some thousand values, to either side.
-        const float d = xs[f] - lo, q = d * inv;
-        const float t1 = fminf(fmaxf(__fmaf_rn(__fmaf_rn(-q, s, d), inv, q), 0.f), kMax);
-        code[2 * e + f] = __float_as_uint(t1 + 12582912.f);   // 1.5 * 2^23: rounds to nearest, ties to even, into the low bits
-      }
-    }
     uint32_t out[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = __byte_perm(code[2 * e], code[2 * e + 1], 0x5410);
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + t * kRowBytes + 16 * part), "r"(out[0]), "r"(out[1]), "r"(out[2]),
-                 "r"(out[3])
+    for (int e = 0; e < 4; ++e) {
+      const float2 v = __half22float2(bits_h2(w[e]));
+      // (x - lo) / s rounded correctly from the rounded reciprocal: one residual and one correction (Markstein, "Computation of
+      // elementary functions on the IBM RISC System/6000 processor", 1990).  A product with the reciprocal alone would move the
+      // ties, which fp16 data meets once in some thousand values, to either side.
+      const float d0 = v.x - lo, d1 = v.y - lo, q0 = d0 * inv, q1 = d1 * inv;
+      const float t0 = __fmaf_rn(__fmaf_rn(-q0, s, d0), inv, q0), t1 = __fmaf_rn(__fmaf_rn(-q1, s, d1), inv, q1);
+      // 1.5 * 2^23 rounds to nearest, ties to even, into the low bits; the greatest code is the limit (s may have been rounded down)
+      out[e] = __vminu2(__byte_perm(__float_as_uint(t0 + 12582912.f), __float_as_uint(t1 + 12582912.f), 0x5410), kBits == 4 ? 0x000f000fu : 0x00ff00ffu);
+    }
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(cell + i * kPer * kRowBytes), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3])
                  : "memory");
     if (valid && part == 0)
       *reinterpret_cast<uint32_t *>(params + 4 * t) = (uint32_t)__half_as_ushort(sh) | ((uint32_t)__half_as_ushort(__float2half_rn(lo)) << 16);
   }
   __syncwarp();
-  uint8_t *const codes = block + (kValue ? kv_code_bytes(kHd, kBits) : 0);
 #pragma unroll
   for (int q = 0; q < kWords / 4; ++q) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < (kBits == 4 ? 4 : 2); ++e) {
-      uint32_t a[4];
-      const uint32_t at = frag_addr<kValue>(tile, kRowBytes, lane, (kBits == 4 ? 4 : 2) * q + e);
-      if (kValue) ldmatrix4_trans(at, a);
+      uint32_t a[4];                                 // keys: (token half, channel half) at 1 and 2; values: (channel half, token half)
+      const uint32_t at = frag_addr(tile, kRowBytes, lane, (kBits == 4 ? 4 : 2) * q + e, value);
+      if (value) ldmatrix4_trans(at, a);
       else ldmatrix4(at, a);
       if (kBits == 4) {
-        if (p.n != kKvBlock) {                       // rows of other tokens hold whatever was there
-#pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] &= 0x000f000fu;
-        }
-        w[e] = kValue ? (a[0] | a[1] << 4 | a[2] << 8 | a[3] << 12) : (a[0] | a[2] << 4 | a[1] << 8 | a[3] << 12);
+        // (the rows of other tokens hold whatever was there)
+        const uint32_t mask = 0x000f000fu, nibble = value ? a[1] : a[2], byte = value ? a[2] : a[1];
+        w[e] = (a[0] & mask) | (nibble & mask) << 4 | (byte & mask) << 8 | (a[3] & mask) << 12;
       } else {
         w[2 * e] = __byte_perm(a[0], a[2], 0x6420), w[2 * e + 1] = __byte_perm(a[1], a[3], 0x6420);
       }
     }
-    uint8_t *const to = codes + 512 * q + 16 * lane;
-    if (p.n == kKvBlock) {
-      *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int t = kv_byte_token<kBits, kValue>(lane, e, j) - p.slot;   // (4 q is even: w's parity is e's)
-          if (t >= 0 && t < p.n) to[4 * e + j] = (uint8_t)(w[e] >> (8 * j));
-        }
+    if (p.n != kKvBlock) {
+      w[0] = (w[0] & ours[0]) | (old[q].x & ~ours[0]), w[1] = (w[1] & ours[1]) | (old[q].y & ~ours[1]);
+      w[2] = (w[2] & ours[0]) | (old[q].z & ~ours[0]), w[3] = (w[3] & ours[1]) | (old[q].w & ~ours[1]);
     }
+    if (ours[0] | ours[1]) *reinterpret_cast<uint4 *>(codes + 512 * q) = make_uint4(w[0], w[1], w[2], w[3]);
   }
   __syncwarp();
 }
@@ -185,7 +214,7 @@ __device__ __forceinline__ void read_block(const KvPiece &p, __half *x, long lon
         const float x1 = fminf(__fmaf_rn(__high2float(c), s[2 * h + 1], lo[2 * h + 1]), 65504.f);
         a[kValue ? q + 2 * h : h + 2 * q] = h2_bits(__floats2half2_rn(x0, x1));
       }
-    const uint32_t at = frag_addr<kValue>(tile, kRowBytes, lane, j);
+    const uint32_t at = frag_addr(tile, kRowBytes, lane, j, kValue);
     if (kValue) stmatrix4_trans(at, a);
     else stmatrix4(at, a);
   }
@@ -221,13 +250,12 @@ __global__ void __launch_bounds__(32 * kWarps) kv_rows_kernel(KvParams p) {
   const int first = blockIdx.x * p.rows_per_cta;
   kv_pieces(p.kv, p.b, kBlockBytes, first, first + p.rows_per_cta, p.status, [&](const KvPiece &piece) {
     uint8_t *const block = p.kv.pages + piece.offset + head_at;
-    if (warp & 1) {
-      if (kWrite) write_block<kHd, kBits, true>(piece, p.v + head * kHd, p.ldv, block, tile);
-      else read_block<kHd, kBits, true>(piece, p.v + head * kHd, p.ldv, block, tile);
-    } else {
-      if (kWrite) write_block<kHd, kBits, false>(piece, p.k + head * kHd, p.ldk, block, tile);
-      else read_block<kHd, kBits, false>(piece, p.k + head * kHd, p.ldk, block, tile);
-    }
+    const bool value = warp & 1;
+    __half *const x = (value ? p.v : p.k) + head * kHd;
+    const long long ldx = value ? p.ldv : p.ldk;
+    if (kWrite) write_block<kHd, kBits>(value, piece, x, ldx, block, tile);
+    else if (value) read_block<kHd, kBits, true>(piece, x, ldx, block, tile);
+    else read_block<kHd, kBits, false>(piece, x, ldx, block, tile);
   });
 }
 

@@ -23,7 +23,7 @@ namespace rosaq {
 //           code * 2^-24 that the tensor core multiplies as they are; (word & 0x00f000f0) the same times 16
 //   8 bits: keys byte 2 p + b of the word of h, values byte 2 h + b of the word of p
 //
-// No byte is shared by two tokens, so tokens are appended with byte stores and no read of what lies around them.
+// No byte is shared by two tokens: what lies around a token is kept by whole bytes.
 // ------------------------------------------------------------------------------------
 constexpr int kKvBlock = 16;                        // tokens of a block
 
@@ -103,7 +103,9 @@ __device__ __forceinline__ void kv_pieces(const KvView &kv, const KvBatchView &b
   first = max(first, b.row_start[0]);
   last = min(last, total);
   if (first >= last) return;
-  int seq = kv_find_seq(b.row_start, b.n_seqs, first);
+  // decoding, a row per sequence: row r is sequence r's, which takes one round of loads to see
+  const int guess = min(first, b.n_seqs - 1);
+  int seq = b.row_start[guess] <= first && first < b.row_start[guess + 1] ? guess : kv_find_seq(b.row_start, b.n_seqs, first);
   for (int row = first; row < last;) {
     while (seq + 1 < b.n_seqs && b.row_start[seq + 1] <= row) ++seq;
     KvPiece p;
