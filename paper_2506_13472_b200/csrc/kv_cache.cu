@@ -54,12 +54,15 @@ __device__ __forceinline__ uint32_t frag_addr(uint32_t tile, int row_bytes, int 
   return tile + tok * row_bytes + 2 * ch;
 }
 
-// (least, minus the greatest) of eight values; kSkip: of those that are numbers, else a NaN where one is
-template <bool kSkip>
-__device__ __forceinline__ __half2 range(const uint32_t *w) {
-  const __half2 a = bits_h2(w[0]), b = bits_h2(w[1]), c = bits_h2(w[2]), d = bits_h2(w[3]);
-  const __half2 lo = kSkip ? __hmin2(__hmin2(a, b), __hmin2(c, d)) : __hmin2_nan(__hmin2_nan(a, b), __hmin2_nan(c, d));
-  const __half2 hi = kSkip ? __hmax2(__hmax2(a, b), __hmax2(c, d)) : __hmax2_nan(__hmax2_nan(a, b), __hmax2_nan(c, d));
+// (least, minus the greatest) of 8 n values; kSkip: of those that are numbers, else a NaN where one is
+template <int n, bool kSkip>
+__device__ __forceinline__ __half2 range(const uint32_t (*w)[4]) {
+  __half2 lo = bits_h2(w[0][0]), hi = lo;
+#pragma unroll
+  for (int i = 1; i < 4 * n; ++i) {
+    const __half2 x = bits_h2(w[i / 4][i % 4]);
+    lo = kSkip ? __hmin2(lo, x) : __hmin2_nan(lo, x), hi = kSkip ? __hmax2(hi, x) : __hmax2_nan(hi, x);
+  }
   const __half l = kSkip ? __hmin(__low2half(lo), __high2half(lo)) : __hmin_nan(__low2half(lo), __high2half(lo));
   const __half h = kSkip ? __hmax(__low2half(hi), __high2half(hi)) : __hmax_nan(__low2half(hi), __high2half(hi));
   return __halves2half2(l, __hneg(h));
@@ -73,12 +76,11 @@ __device__ __forceinline__ void write_block(bool value, const KvPiece &p, const 
   constexpr int kWords = kHd / 16 * (kBits / 4);
   constexpr float kMax = kBits == 4 ? 15.f : 255.f;
   const int lane = threadIdx.x & 31, part = lane % kLanes, mine = lane / kLanes;
-  const uint32_t cell = tile + mine * kRowBytes + 16 * part;   // this lane's 16 bytes of the first step's tokens: values, then 16-bit codes
-  // ---- the rows, as far as shared memory; every lane uses what it has brought itself
+  // ---- the rows, as far as shared memory
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int t = i * kPer + mine - p.slot;
-    if (t >= 0 && t < p.n) copy16(cell + i * kPer * kRowBytes, x + (p.row + t) * ldx + 8 * part);
+    if (t >= 0 && t < p.n) copy16(tile + (i * kPer + mine) * kRowBytes + 16 * part, x + (p.row + t) * ldx + 8 * part);
   }
   uint8_t *const codes = block + (value ? kv_code_bytes(kHd, kBits) : 0) + 16 * lane;
   // which bytes of this lane's words (even and odd ones) are this piece's, and what is there now
@@ -99,52 +101,63 @@ __device__ __forceinline__ void write_block(bool value, const KvPiece &p, const 
       if (ours[0] | ours[1]) old[q] = *reinterpret_cast<const uint4 *>(codes + 512 * q);
   }
   copy_wait_all();
+  __syncwarp();
   uint8_t *const params = block + 2 * kv_code_bytes(kHd, kBits) + (value ? 4 * kKvBlock : 0);
+  // ---- codes in the values' place.  Four lanes per token, each every fourth 16 bytes: what a token costs besides its values (two divisions, the exchange) is shared by 32
+  // of them (2048 rows x 32 heads: 15.9 us with sixteen lanes per token)
+  const int quad = lane & 3;
 #pragma unroll 1
-  for (int i = p.slot / kPer; i * kPer < p.slot + p.n; ++i) {
-    const int t = i * kPer + mine;
+  for (int t0 = p.slot & ~7; t0 < p.slot + p.n; t0 += 8) {
+    const int t = t0 + (lane >> 2);
     const bool valid = t >= p.slot && t < p.slot + p.n;
-    const uint4 in = valid ? lds128(cell + i * kPer * kRowBytes) : make_uint4(0, 0, 0, 0);
-    uint32_t w[4] = {in.x, in.y, in.z, in.w};
+    const uint32_t cell = tile + t * kRowBytes + 16 * quad;
+    uint32_t w[kHd / 32][4];
+#pragma unroll
+    for (int k = 0; k < kHd / 32; ++k) {
+      const uint4 v = lds128(cell + 64 * k);         // (of tokens that are not this piece's: whatever was there)
+      w[k][0] = v.x, w[k][1] = v.y, w[k][2] = v.z, w[k][3] = v.w;
+    }
     // (least, minus the greatest).  Almost always all are numbers: NaNs come through this way, and what is not finite is seen to apart.
-    __half2 m = range<false>(w);
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d /= 2) m = __hmin2_nan(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), d)));
+    __half2 m = range<kHd / 32, false>(w);
+    m = __hmin2_nan(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), 1))), m = __hmin2_nan(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), 2)));
     float lo = __low2float(m), hi = -__high2float(m);
-    if (__any_sync(0xffffffffu, !(lo >= -65504.f && hi <= 65504.f))) {
-      m = range<true>(w);                            // a NaN is in neither
-#pragma unroll
-      for (int d = kLanes / 2; d > 0; d /= 2) m = __hmin2(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), d)));
+    if (__any_sync(0xffffffffu, valid && !(lo >= -65504.f && hi <= 65504.f))) {
+      m = range<kHd / 32, true>(w);                  // a NaN is in neither
+      m = __hmin2(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), 1))), m = __hmin2(m, bits_h2(__shfl_xor_sync(0xffffffffu, h2_bits(m), 2)));
       lo = __low2float(m), hi = -__high2float(m);
       if (isnan(lo)) lo = hi = 0.f;
       lo = fminf(fmaxf(lo, -65504.f), 65504.f), hi = fminf(fmaxf(hi, -65504.f), 65504.f);
       // infinities end up at the ends of the range, a NaN at its least value
       const __half2 least = __float2half2_rn(lo);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const __half2 c = __hmin2(__hmax2(bits_h2(w[e]), bits_h2(0xfbfffbffu)), bits_h2(0x7bff7bffu));
-        w[e] = h2_bits(__hmax2(c, least));           // (a NaN came out of the two before as -65504)
-      }
+      for (int k = 0; k < kHd / 32; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __half2 c = __hmin2(__hmax2(bits_h2(w[k][e]), bits_h2(0xfbfffbffu)), bits_h2(0x7bff7bffu));
+          w[k][e] = h2_bits(__hmax2(c, least));      // (a NaN came out of the two before as -65504)
+        }
     }
     lo += 0.f;                                       // (no negative zero)
     __half sh = __float2half_rn(__fdiv_rn(hi - lo, kMax));
     if (__half_as_ushort(sh) == 0) sh = __ushort_as_half(1);
     const float s = __half2float(sh), inv = __frcp_rn(s);
-    uint32_t out[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 v = __half22float2(bits_h2(w[e]));
-      // (x - lo) / s rounded correctly from the rounded reciprocal: one residual and one correction (Markstein, "Computation of
-      // elementary functions on the IBM RISC System/6000 processor", 1990).  A product with the reciprocal alone would move the
-      // ties, which fp16 data meets once in some thousand values, to either side.
-      const float d0 = v.x - lo, d1 = v.y - lo, q0 = d0 * inv, q1 = d1 * inv;
-      const float t0 = __fmaf_rn(__fmaf_rn(-q0, s, d0), inv, q0), t1 = __fmaf_rn(__fmaf_rn(-q1, s, d1), inv, q1);
-      // 1.5 * 2^23 rounds to nearest, ties to even, into the low bits; the greatest code is the limit (s may have been rounded down)
-      out[e] = __vminu2(__byte_perm(__float_as_uint(t0 + 12582912.f), __float_as_uint(t1 + 12582912.f), 0x5410), kBits == 4 ? 0x000f000fu : 0x00ff00ffu);
+    for (int k = 0; k < kHd / 32; ++k) {
+      uint32_t out[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 v = __half22float2(bits_h2(w[k][e]));
+        // (x - lo) / s rounded correctly from the rounded reciprocal: one residual and one correction (Markstein, "Computation of
+        // elementary functions on the IBM RISC System/6000 processor", 1990).  A product with the reciprocal alone would move the
+        // ties, which fp16 data meets once in some thousand values, to either side.
+        const float d0 = v.x - lo, d1 = v.y - lo, q0 = d0 * inv, q1 = d1 * inv;
+        const float u0 = __fmaf_rn(__fmaf_rn(-q0, s, d0), inv, q0), u1 = __fmaf_rn(__fmaf_rn(-q1, s, d1), inv, q1);
+        // 1.5 * 2^23 rounds to nearest, ties to even, into the low bits; the greatest code is the limit (s may have been rounded down)
+        out[e] = __vminu2(__byte_perm(__float_as_uint(u0 + 12582912.f), __float_as_uint(u1 + 12582912.f), 0x5410), kBits == 4 ? 0x000f000fu : 0x00ff00ffu);
+      }
+      asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(cell + 64 * k), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
     }
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(cell + i * kPer * kRowBytes), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3])
-                 : "memory");
-    if (valid && part == 0)
+    if (valid && quad == 0)
       *reinterpret_cast<uint32_t *>(params + 4 * t) = (uint32_t)__half_as_ushort(sh) | ((uint32_t)__half_as_ushort(__float2half_rn(lo)) << 16);
   }
   __syncwarp();
