@@ -28,7 +28,10 @@ namespace {
 
 constexpr int kChunk = 2, kTokens = kChunk * kKvBlock;   // blocks that a warp takes at a time
 constexpr int kRows = 8;                            // query rows of a tile
-constexpr long long kManyRows = 1ll << 40;          // per sequence and key/value head: from here on attend_rows.cu
+#ifndef MANY
+#define MANY 64
+#endif
+constexpr long long kManyRows = MANY;          // per sequence and key/value head: from here on attend_rows.cu
 
 __device__ __forceinline__ float lg2(float x) {
   float y;

@@ -61,6 +61,11 @@ __device__ __forceinline__ uint32_t pack_h2(float a, float b) {
   return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+__device__ __forceinline__ uint32_t h2_fma(uint32_t v, uint32_t mul, uint32_t add) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&mul), *reinterpret_cast<const __half2 *>(&add));
+  return *reinterpret_cast<const uint32_t *>(&r);
+}
+
 // The next chunk of a walk over the list: sequence, (head, tile) in it, chunk of that.
 struct Cursor {
   int seq, unit, chunk;

@@ -1,4 +1,445 @@
+// rosaq_attend for many query rows per sequence and key/value head: a prompt, or a batch behind a shared prefix.
+//
+// Bound: the tensor core, so it is tcgen05 here: per chunk of 64 tokens S = Q K^T (128 rows x 64 tokens, both operands in shared memory) and O += P V (P in tensor memory over its
+// scores, V in shared memory), fp32 accumulators in tensor memory.  A CTA has up to two tiles of 128 rows, which share every key and value that four warps make of the codes:
+// lo + scale * code in one fp16 fused multiply-add, i.e. rounded once to fp16 (2^-11; as are the softmax weights), in the fragment order of the cache's words, so that one stmatrix
+// stores four 8 x 8 pieces: rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  While the tensor core
+// works on one tile's chunk, four warps do the softmax of the other's, a row per thread; the scores of the next chunk go to a second buffer.  The maximum of a row is renewed only
+// when it is exceeded by 2^8: then its accumulators are rescaled in tensor memory.
+//
+// Per chunk and pair of tiles: 1056 cycles of MMA, 1024 of exponentials (16 per cycle and SM), about 1000 issue slots of the four schedulers.
+#include <algorithm>
+
 #include "attend_common.cuh"
+
 namespace rosaq {
-int launch_attend_rows(rosaq_ctx *, AtParams, int, int, cudaStream_t) { return ROSAQ_ERR_UNSUPPORTED_SHAPE; }
+namespace {
+
+constexpr int kTile = 128, kRows = 2 * kTile;       // query rows of an MMA, of a CTA's tile
+constexpr int kTokens = 64, kBlocks = kTokens / kKvBlock;
+constexpr int kWorkers = 8;                         // softmax warps
+constexpr int kConsumers = 32 * kWorkers, kMakers = 4;
+constexpr int kThreads = 32 * (kWorkers + kMakers + 2);
+
+template <int kHd, int kBits>
+struct RCfg {
+  static constexpr int kHalves = kHd / 64;          // 64 channels: a row of 128 bytes
+  static constexpr int kQBytes = kTile * 2 * kHd, kKBytes = kTokens * 2 * kHd, kVBytes = kKBytes;
+  static constexpr int kRawBytes = kBlocks * kv_block_bytes(kHd, kBits);
+  static constexpr int kRaw = 3;                    // chunks of codes under way
+  static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + 2 * kKBytes, kOffRaw = kOffV + 2 * kVBytes, kOffBars = kOffRaw + kRaw * kRawBytes;
+  static constexpr int kSmem = kOffBars + 512 + 1024;   // (the swizzled operands start at a multiple of 1024)
+  static constexpr long long kWorkBytes = 2 * 4 * at_partial(kHd, kRows);   // of a CTA
+};
+// barriers
+constexpr int kRawFull = 0, kRawEmpty = 4, kKvFull = 8, kKFree = 10, kVFree = 12, kSFull = 14 /* [tile][buffer] */, kPFull = 18, kODone = 22 /* [tile] */, kQFull = 24, kDone = 26, kBars = 27;
+// tensor memory
+__device__ __forceinline__ uint32_t s_col(int tile, int buf) { return 128 * tile + 64 * buf; }
+__device__ __forceinline__ uint32_t o_col(int tile) { return 256 + 128 * tile; }
+
+__device__ __forceinline__ void stmatrix4(uint32_t addr, const uint32_t *a) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3])
+               : "memory");
 }
+// D (+)= A B over 64 of k: four MMAs, both operands K-major in shared memory (A: 128 rows; rows of 128 bytes, swizzled)
+__device__ __forceinline__ void mma4_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q, e;\n\t.reg .b64 ta, tb;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 q, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "add.u64 ta, %1, 2;\n\tadd.u64 tb, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], ta, tb, %3, q;\n\t"
+      "add.u64 ta, %1, 4;\n\tadd.u64 tb, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], ta, tb, %3, q;\n\t"
+      "add.u64 ta, %1, 6;\n\tadd.u64 tb, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], ta, tb, %3, q;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// the same with A in tensor memory: 16 of k are eight columns
+__device__ __forceinline__ void mma4_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q, e;\n\t.reg .b64 tb;\n\t.reg .b32 ta;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 q, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "add.u32 ta, %1, 8;\n\tadd.u64 tb, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], tb, %3, q;\n\t"
+      "add.u32 ta, %1, 16;\n\tadd.u64 tb, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], tb, %3, q;\n\t"
+      "add.u32 ta, %1, 24;\n\tadd.u64 tb, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], tb, %3, q;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// the chunks of a tile that a CTA goes through, and what it may skip: everything behind the last token that a row sees
+struct Segment {
+  int head, tile, chunk0, count, rows;              // count: chunks that are worked on (none: nothing is seen)
+  bool whole;
+};
+__device__ __forceinline__ Segment segment(const AtParams &p, const Cursor &c, int left) {
+  Segment g;
+  const Seq &s = c.s;
+  g.head = c.unit / s.tiles, g.tile = c.unit - g.head * s.tiles, g.chunk0 = c.chunk;
+  const int first_row = g.tile * kRows, n_flat = s.rows * p.group;
+  g.rows = min(kRows, n_flat - first_row);
+  const int take = min(left, s.chunks - c.chunk);
+  g.whole = c.chunk == 0 && take == s.chunks;
+  int seen = s.len;
+  if (p.prefix_tokens == 0) seen = min(max(s.len - s.rows + 1 + (first_row + g.rows - 1) / p.group, 0), s.len);
+  g.count = min(take, max((seen + kTokens - 1) / kTokens - c.chunk, 0));
+  return g;
+}
+
+template <int kHd, int kBits>
+__global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_constant__ AtParams p) {
+  using C = RCfg<kHd, kBits>;
+  constexpr int kWords = kHd / 16 * (kBits / 4), kBlockBytes = kv_block_bytes(kHd, kBits);
+  extern __shared__ uint8_t dyn[];
+  uint8_t *const smem = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
+  const uint32_t base = smem_u32(smem), bars = base + C::kOffBars;
+  OpenTile *const open = reinterpret_cast<OpenTile *>(smem + C::kOffBars + 8 * kBars);   // [2] tiles that other CTAs hold parts of too
+  int *const span = reinterpret_cast<int *>(open + 2);
+  uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(span + 4);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return bars + 8 * i; };
+
+  Share share;
+  if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, 16, 4, blockIdx.x == 0 && warp == 0, share)) return;
+  Cursor cur = share.cur;
+  const int n = (int)(share.end - share.begin);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kRaw; ++i) mbar_init(bar(kRawFull + i), 1), mbar_init(bar(kRawEmpty + i), kMakers);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(kKvFull + i), kMakers), mbar_init(bar(kKFree + i), 1), mbar_init(bar(kVFree + i), 1);
+      mbar_init(bar(kODone + i), 1), mbar_init(bar(kQFull + i), 4);
+      for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4);
+    }
+    mbar_init(bar(kDone), 1);
+    mbar_init_fence();
+    open[0].from = open[1].from = kNoTile;
+  }
+  if (warp == kWorkers + kMakers) tmem_alloc<512>(smem_u32(tmem_at));
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_at;
+
+  // A wait that expires is reported, and the warp waits no more: it goes on through what the others rely on.
+  bool lost = false;
+  auto wait = [&](int b, uint32_t parity) {
+    if (lost) return;
+    bool here = mbar_try_wait(bar(b), parity);
+    if (!__all_sync(0xffffffffu, here)) {
+      for (long long i = 0; !here && i < p.wait_limit; ++i) here = mbar_try_wait(bar(b), parity);
+      lost = !__all_sync(0xffffffffu, here);
+      if (lost && lane == 0) atomicExch(p.status, (int)ROSAQ_ERR_TIMEOUT);
+    }
+  };
+
+  if (warp < kWorkers) {
+    // ================================================================ softmax: warps 0-3 the first tile, 4-7 the second; a row per thread
+    const int x = warp >> 2, row = 32 * (warp & 3) + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    const float a = fmaxf(fabsf(p.scale_log2), 1e-30f);   // (its sign is in the queries)
+    const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : p.scale_log2 == 0.f ? 0.f : 1.f);
+    uint32_t g = 0;                                  // chunks of this tile so far
+    for (int left = n; left > 0;) {
+      settle<kRows, kTokens>(p, cur);
+      const Segment sg = segment(p, cur, left);
+      const Seq &s = cur.s;
+      const int take = min(left, s.chunks - cur.chunk), flat = sg.tile * kRows + kTile * x + row;
+      const bool active = sg.rows > kTile * x, valid = kTile * x + row < sg.rows;
+      const int tok = valid ? flat / p.group : 0;
+      float top = kNone, den = 0.f;
+      if (active && sg.count > 0) {
+        // ---- the queries
+        const __half *const src = p.q + (long long)(s.row + tok) * p.ldq + (long long)(sg.head * p.group + (valid ? flat - tok * p.group : 0)) * kHd;
+        uint8_t *const q = smem + x * C::kQBytes + 128 * row;
+#pragma unroll
+        for (int k = 0; k < kHd / 8; ++k) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (valid) v = *reinterpret_cast<const uint4 *>(src + 8 * k);
+          __half2 *const h = reinterpret_cast<__half2 *>(&v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = __hmul2(h[e], sign);
+          *reinterpret_cast<uint4 *>(q + (k / 8) * (128 * kTile) + (((k & 7) ^ (row & 7)) << 4)) = v;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kQFull + x));
+        const int lim = p.prefix_tokens > 0 ? s.len : valid ? min(max(s.len - s.rows + 1 + tok, 0), s.len) : s.len;
+        const int least = __reduce_min_sync(0xffffffffu, lim);
+        for (int j = 0; j < sg.count; ++j, ++g) {
+          const int buf = g & 1, tok0 = (sg.chunk0 + j) * kTokens;
+          bool through = j == 0;                     // the product before this one is
+          wait(kSFull + 2 * x + buf, (g >> 1) & 1);
+          tc_fence_after();
+          float sc[kTokens];
+#pragma unroll
+          for (int i = 0; i < kTokens / 16; ++i) tmem_ld16(lanes + s_col(x, buf) + 16 * i, reinterpret_cast<uint32_t *>(sc + 16 * i));
+          tc_wait_ld();
+          if (tok0 + kTokens > least) {
+#pragma unroll
+            for (int i = 0; i < kTokens; ++i)
+              if (tok0 + i >= lim) sc[i] = -INFINITY;
+          }
+          float m[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) m[i] = fmaxf(sc[i], sc[i + 4]);
+#pragma unroll
+          for (int i = 8; i < kTokens; i += 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], sc[i + e]);
+          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a;
+          if (__any_sync(0xffffffffu, most > top + kGrow)) {
+            const float now = fmaxf(most, top), f = ex2(top - now);
+            top = now, den *= f;
+            if (j > 0) {
+              wait(kODone + x, (g - 1) & 1), through = true;
+              tc_fence_after();
+#pragma unroll 1
+              for (int i = 0; i < kHd; i += 16) {
+                float o[16];
+                tmem_ld16(lanes + o_col(x) + i, reinterpret_cast<uint32_t *>(o));
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f;
+                tmem_st16(lanes + o_col(x) + i, reinterpret_cast<const uint32_t *>(o));
+              }
+            }
+          }
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          uint32_t w[kTokens / 2];
+#pragma unroll
+          for (int i = 0; i < kTokens / 2; ++i) {
+            const float u = ex2(__fmaf_rn(sc[2 * i], a, -top)), v = ex2(__fmaf_rn(sc[2 * i + 1], a, -top));
+            sum[2 * (i & 1)] += u, sum[2 * (i & 1) + 1] += v;
+            w[i] = pack_h2(u, v);
+          }
+          den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          // the weights over the first half of the scores
+          tmem_st16(lanes + s_col(x, buf), w);
+          tmem_st16(lanes + s_col(x, buf) + 16, w + 16);
+          tc_wait_st();
+          // (every phase of that barrier is waited for, before the next one can end)
+          if (!through) wait(kODone + x, (g - 1) & 1);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(kPFull + 2 * x + buf));
+        }
+        wait(kODone + x, (g - 1) & 1);
+        tc_fence_after();
+      }
+      // ---- the rows, or this CTA's part of them
+      const int from = n - left - sg.chunk0;
+      if (active) {
+        const int r = kTile * x + row;
+        float *const part = my_partial(p, from, at_partial(kHd, kRows));
+        const RowAt to = row_at<kHd>(p, s.row, sg.head, valid ? flat : 0);
+#pragma unroll 1
+        for (int i = 0; i < kHd; i += 16) {
+          float o[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = 0.f;
+          if (sg.count > 0) {
+            tmem_ld16(lanes + o_col(x) + i, reinterpret_cast<uint32_t *>(o));
+            tc_wait_ld();
+          }
+          if (!valid) continue;
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 v = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            if (sg.whole) store_row4<kHd>(p, to, i + e, v, top, den);
+            else *reinterpret_cast<float4 *>(part + r * kHd + i + e) = v;
+          }
+        }
+        if (valid && !sg.whole) *reinterpret_cast<float2 *>(part + kRows * kHd + 2 * r) = make_float2(top, den);
+      }
+      if (!sg.whole && threadIdx.x == 0) open[from < 0 ? 0 : 1] = OpenTile{from, cur.seq, cur.unit, s.chunks};
+      tc_fence_before();
+      left -= take, cur.chunk += take;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory");
+    // (the queries are not needed any more)
+    join_shares<kHd, kRows, kTokens, kConsumers>(p, share.all, share.begin, open, span, reinterpret_cast<float4 *>(smem));
+  } else if (warp < kWorkers + kMakers) {
+    // ================================================================ keys and values from codes: a block of sixteen tokens per warp
+    const int blk = warp - kWorkers, r = lane >> 2, c = lane & 3;
+    // where stmatrix puts the four pieces of a step: this lane names row lane & 7 of piece lane >> 3
+    const int h1 = (lane >> 3) & 1, h2 = lane >> 4;
+    uint32_t g = 0;
+    for (int left = n; left > 0;) {
+      settle<kRows, kTokens>(p, cur);
+      const Segment sg = segment(p, cur, left);
+      const int take = min(left, cur.s.chunks - cur.chunk);
+      for (int j = 0; j < sg.count; ++j, ++g) {
+        const int st = g & 1, raw = g % C::kRaw;
+        const uint32_t from = base + C::kOffRaw + raw * C::kRawBytes + blk * kBlockBytes;
+        const int tok0 = (sg.chunk0 + j) * kTokens + blk * kKvBlock;
+        wait(kRawFull + raw, (g / C::kRaw) & 1);
+        if (g >= 2) wait(kKFree + st, (g / 2 - 1) & 1), wait(kVFree + st, (g / 2 - 1) & 1);
+        // scale and least value; zeros behind the last token, whatever lies there.  (A group that reaches to the end of fp16 may pass it with its greatest code: the
+        // scale is a step smaller then.)
+        auto pair = [&](uint32_t at, int tok) {
+          uint32_t v = lds32(at);
+          const float2 f = __half22float2(*reinterpret_cast<__half2 *>(&v));
+          if (__fmaf_rn(f.x, kBits == 4 ? 15.f : 255.f, f.y) > 65504.f) v -= 1;
+          return tok < cur.s.len ? v : 0u;
+        };
+        constexpr int kPairs = 2 * kv_code_bytes(kHd, kBits);
+#pragma unroll
+        for (int value = 0; value < 2; ++value) {
+          uint32_t sc[2], lo[2];                     // keys: of tokens r and r + 8, twice each; values: of tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int t = value ? 8 * h + 2 * c : 8 * h + r;
+            const uint32_t u = pair(from + kPairs + 64 * value + 4 * t, tok0 + t), v = value ? pair(from + kPairs + 64 * value + 4 * t + 4, tok0 + t + 1) : u;
+            sc[h] = __byte_perm(u, v, 0x5410), lo[h] = __byte_perm(u, v, 0x7632);
+          }
+          uint32_t to;                               // of step 0; keys advance by two 16-byte pieces of a row, values by sixteen rows
+          if (value) to = base + C::kOffV + st * C::kVBytes + 128 * (8 * h1 + (lane & 7)) + (((2 * blk + h2) ^ (lane & 7)) << 4);
+          else to = base + C::kOffK + st * C::kKBytes + 128 * (kKvBlock * blk + 8 * h1 + (lane & 7));
+#pragma unroll
+          for (int i = 0; i < kWords / 4; ++i) {
+            const uint4 v4 = lds128(from + value * kv_code_bytes(kHd, kBits) + 512 * i + 16 * lane);
+            const uint32_t w[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+            for (int e = 0; e < (kBits == 4 ? 4 : 2); ++e) {
+              const int k = (kBits == 4 ? 4 : 2) * i + e;
+              uint32_t f[4];                         // codes; pieces in the order (row half, k half) = (0, 0), (1, 0), (0, 1), (1, 1)
+              if (kBits == 4) {
+                constexpr uint32_t kOne = 0x3c003c00u, kSixteenth = 0x2c002c00u, kLow = 0xe400e400u, kHigh = 0xd400d400u;   // -1024, -64
+                const uint32_t u = w[e], v = u >> 8;
+                const uint32_t n0 = h2_fma(lop_and_or(u, 0x000f000fu, 0x64006400u), kOne, kLow), n1 = h2_fma(lop_and_or(u, 0x00f000f0u, 0x64006400u), kSixteenth, kHigh);
+                const uint32_t n2 = h2_fma(lop_and_or(v, 0x000f000fu, 0x64006400u), kOne, kLow), n3 = h2_fma(lop_and_or(v, 0x00f000f0u, 0x64006400u), kSixteenth, kHigh);
+                f[0] = n0, f[1] = value ? n1 : n2, f[2] = value ? n2 : n1, f[3] = n3;
+              } else {
+                constexpr uint32_t kOne = 0x3c003c00u, kMid = 0xe400e400u;
+                const uint32_t u = w[2 * e], v = w[2 * e + 1];
+                f[0] = h2_fma(__byte_perm(u, 0x64646464u, 0x4140), kOne, kMid), f[1] = h2_fma(__byte_perm(v, 0x64646464u, 0x4140), kOne, kMid);
+                f[2] = h2_fma(__byte_perm(u, 0x64646464u, 0x4342), kOne, kMid), f[3] = h2_fma(__byte_perm(v, 0x64646464u, 0x4342), kOne, kMid);
+              }
+              // keys: rows are tokens, values: k is
+              f[0] = h2_fma(f[0], sc[0], lo[0]), f[1] = h2_fma(f[1], sc[value ? 0 : 1], lo[value ? 0 : 1]);
+              f[2] = h2_fma(f[2], sc[value ? 1 : 0], lo[value ? 1 : 0]), f[3] = h2_fma(f[3], sc[1], lo[1]);
+              if (value) stmatrix4(to + 2048 * k, f);
+              else stmatrix4(to + (k / 4) * (128 * kTokens) + ((((2 * k + h2) & 7) ^ (lane & 7)) << 4), f);
+            }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kKvFull + st)), mbar_arrive(bar(kRawEmpty + raw));
+      }
+      left -= take, cur.chunk += take;
+    }
+  } else if (warp == kWorkers + kMakers) {
+    // ================================================================ MMAs
+    const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
+    uint32_t g = 0, gx[2] = {0, 0}, segs[2] = {0, 0};
+    for (int left = n; left > 0;) {
+      settle<kRows, kTokens>(p, cur);
+      const Segment sg = segment(p, cur, left);
+      const int take = min(left, cur.s.chunks - cur.chunk), tiles = sg.rows > kTile ? 2 : 1;
+      auto scores = [&](int j) {                     // of chunk j of the segment
+        const uint32_t at = g + j;
+        wait(kKvFull + (at & 1), (at >> 1) & 1);
+        tc_fence_after();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x >= tiles) continue;
+          const uint32_t gj = gx[x] + j;
+          if (!lost)
+#pragma unroll
+            for (int h = 0; h < C::kHalves; ++h)
+              mma4_ss(tmem + s_col(x, gj & 1), make_b_desc(base + x * C::kQBytes + h * 128 * kTile), make_b_desc(base + C::kOffK + (at & 1) * C::kKBytes + h * 128 * kTokens),
+                      idesc_s, h);
+          tc_commit(bar(kSFull + 2 * x + (gj & 1)));
+        }
+        tc_commit(bar(kKFree + (at & 1)));
+      };
+      if (sg.count > 0) {
+        for (int x = 0; x < tiles; ++x) wait(kQFull + x, segs[x]++ & 1);
+        scores(0);
+        for (int j = 0; j < sg.count; ++j) {
+          if (j + 1 < sg.count) scores(j + 1);
+          const uint32_t at = g + j;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= tiles) continue;
+            const uint32_t gj = gx[x] + j;
+            wait(kPFull + 2 * x + (gj & 1), (gj >> 1) & 1);
+            tc_fence_after();
+            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, gj & 1), make_b_desc(base + C::kOffV + (at & 1) * C::kVBytes), idesc_o, j > 0);
+            tc_commit(bar(kODone + x));
+          }
+          tc_commit(bar(kVFree + (at & 1)));
+        }
+        g += sg.count, gx[0] += sg.count;
+        if (tiles == 2) gx[1] += sg.count;
+      }
+      left -= take, cur.chunk += take;
+    }
+    // everything issued is over before the tensor memory is given back, whatever was waited for
+    tc_commit(bar(kDone));
+    for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kDone), 0); ++i) {}
+  } else {
+    // ================================================================ copies: lane i brings block i of the chunk
+    uint32_t g = 0;
+    const uint64_t keep = policy_evict_first();
+    for (int left = n; left > 0;) {
+      settle<kRows, kTokens>(p, cur);
+      const Segment sg = segment(p, cur, left);
+      const int take = min(left, cur.s.chunks - cur.chunk);
+      const uint8_t *const heads = p.kv.pages + ((long long)sg.head << p.kv.page_shift) * kBlockBytes;
+      for (int j = 0; j < sg.count && !lost; ++j, ++g) {
+        const int raw = g % C::kRaw, block = (sg.chunk0 + j) * kBlocks, blocks = min(kBlocks, (cur.s.len + kKvBlock - 1) / kKvBlock - block);
+        // runs of blocks of a page: one copy per run, by the lane of its first block
+        const int run = min(1 << p.kv.page_shift, kBlocks);
+        const bool mine = lane < blocks && lane % run == 0;
+        int page = 0;
+        if (mine) page = kv_page(p.kv, p.b, cur.seq, block + lane);
+        if (page < 0) kv_report(p.status), page = 0;         // (the first page of the cache in its place)
+        if (g >= (uint32_t)C::kRaw) wait(kRawEmpty + raw, (g / C::kRaw - 1) & 1);
+        if (lost) break;
+        if (lane == 0) mbar_arrive_expect_tx(bar(kRawFull + raw), blocks * kBlockBytes);
+        __syncwarp();
+        if (mine)
+          bulk_copy_g2s_hint(base + C::kOffRaw + raw * C::kRawBytes + lane * kBlockBytes, heads + kv_offset(p.kv, page, block + lane, kBlockBytes),
+                             min(run, blocks - lane) * kBlockBytes, bar(kRawFull + raw), keep);
+      }
+      left -= take, cur.chunk += take;
+    }
+    // the CTA outlasts its copies, also when nobody waits for them any more
+    for (uint32_t k = g < (uint32_t)C::kRaw ? 0 : g - C::kRaw; k < g; ++k)
+      for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) {}
+  }
+  __syncthreads();
+  if (warp == kWorkers + kMakers) tmem_dealloc<512>(tmem);
+}
+
+template <int kHd, int kBits>
+int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
+  using C = RCfg<kHd, kBits>;
+  static_assert(C::kSmem <= 227 * 1024 && 8 * kBars + 2 * sizeof(OpenTile) + 32 <= 512 && 32 * kConsumers <= 2 * C::kQBytes, "shared memory");
+  auto *const kern = attend_rows_kernel<kHd, kBits>;
+  int &ready = ctx->at_per_sm[4 + (kHd == 64) + 2 * (kBits == 8)];
+  if (ready == 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return ROSAQ_ERR_CUDA;
+  }
+  ready = 1;
+  const int ctas = std::min(ctx->sm_count, kAtMaxCtas);
+  const int st = grow_workspace(ctx, reinterpret_cast<void **>(&ctx->at_partials), &ctx->at_partial_bytes, (size_t)(ctas * C::kWorkBytes));
+  if (st != ROSAQ_OK) return st;
+  p.partials = ctx->at_partials;
+  // Not chained to the launch before it: a CTA takes all of an SM's tensor memory, which a CTA of that launch may still be going to ask for.
+  kern<<<ctas, kThreads, C::kSmem, s>>>(p);
+  if (cudaGetLastError() != cudaSuccess) return ROSAQ_ERR_CUDA;
+  return ROSAQ_OK;
+}
+
+}  // namespace
+
+int launch_attend_rows(rosaq_ctx *ctx, AtParams p, int hd, int bits, cudaStream_t s) {
+  if (hd == 128) return bits == 4 ? launch<128, 4>(ctx, p, s) : launch<128, 8>(ctx, p, s);
+  return bits == 4 ? launch<64, 4>(ctx, p, s) : launch<64, 8>(ctx, p, s);
+}
+
+}  // namespace rosaq

@@ -292,7 +292,7 @@ struct rosaq_ctx {
   float *at_prefix;                              // what a batch found in its shared prefix, grown on demand
   size_t at_prefix_bytes;
   int *at_arrived;                               // [kAtMaxCtas] CTAs that have stored their partial tile; zero between launches
-  int at_per_sm[4];                              // resident CTAs per SM of each variant (0 until first asked for)
+  int at_per_sm[8];                              // of each variant, resident CTAs per SM (0 until first asked for)
   unsigned *pf_flags;                            // [pair][2][rank]: readers that have yet to fetch a partial tile; zero between launches
 };
 

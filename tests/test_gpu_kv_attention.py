@@ -207,6 +207,9 @@ def fill(ctx, rng, held, table, lens, loud=1.0, v_size=1.0, offset=0.0):
 
 def expect(held, table, lens, new, q, scale, prefix=None):
     """(out, bound) of all rows."""
+    group = q.shape[1] // held.width
+    many = lambda rows: rows * group >= 64  # noqa: E731   (from here on the kernel that rounds keys and values to fp16)
+    rounded = many(-(-q.shape[0] // len(lens))) or (prefix is not None and many(q.shape[0]))
     outs, bounds, at = [], [], 0
     hd, hq = held.head_dim, q.shape[1] // held.head_dim
     args = (held.pages, held.n_kv_heads, hd, held.bits, held.page_tokens)
@@ -218,7 +221,7 @@ def expect(held, table, lens, new, q, scale, prefix=None):
         if pre:
             kv = [[torch.cat([a, b]) for a, b in zip(x, y)] for x, y in zip(pre, kv)]
         seen = torch.arange(np_ + n, device="cuda")[None, :] < np_ + n - m + 1 + torch.arange(m, device="cuda")[:, None]
-        o, b = ref.attention(q[at:at + m].double().view(m, hq, hd), kv, seen, scale)
+        o, b = ref.attention(q[at:at + m].double().view(m, hq, hd), kv, seen, scale, rounded)
         outs.append(o.reshape(m, -1)), bounds.append(b.reshape(m, -1))
         at += m
     return torch.cat(outs), torch.cat(bounds)
