@@ -417,9 +417,12 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
           for (int k = 0; k < kSteps; ++k) to.prefix[16 * k + r] = acc[k][e] + off[e], to.prefix[16 * k + 8 + r] = acc[k][e + 2] + off[e];
           if (r == 0) *reinterpret_cast<float2 *>(to.prefix + kHd) = make_float2(top[e], l);
         } else {
-          float f = 1.f, g = 0.f;
+          // (the prefix's sums before the first store, which might be to the same memory for all the compiler knows: one trip, not 32)
+          float f = 1.f, g = 0.f, pre[kSteps][2];
           if (to.prefix) {
             const float2 ml = *reinterpret_cast<const float2 *>(to.prefix + kHd);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) pre[k][0] = to.prefix[16 * k + r], pre[k][1] = to.prefix[16 * k + 8 + r];
             const float mm = fmaxf(top[e], ml.x);
             f = ex2(top[e] - mm), g = ex2(ml.x - mm);
             l = l * f + ml.y * g;
@@ -431,7 +434,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float x = (acc[k][e + 2 * h] + off[e]) * f;
-              if (to.prefix) x = __fmaf_rn(to.prefix[16 * k + 8 * h + r], g, x);
+              if (to.prefix) x = __fmaf_rn(pre[k][h], g, x);
               to.out[16 * k + 8 * h + r] = __float2half_rn(x);
             }
         }

@@ -232,12 +232,42 @@ __device__ __forceinline__ float *my_partial(const AtParams &p, int from, int fl
   return p.partials + (2ll * blockIdx.x + (from < 0 ? 0 : 1)) * floats;
 }
 
+// Adds the parts of CTAs first, first + step, ... c1 of a row's channels ch ... ch + 3; the tile begins in CTA c0's share.
+template <int kHd, int kRows>
+__device__ __forceinline__ void gather(const AtParams &p, int row, int ch, int c0, int c1, int first, int step, float4 &a, float &m, float &l) {
+  constexpr int kAhead = 8;                      // loads in flight
+  for (int k = first; k <= c1; k += kAhead * step) {
+    float4 x[kAhead];
+    float2 ml[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int kk = k + u * step;
+      const float *const from = p.partials + (2ll * kk + (kk == c0)) * at_partial(kHd, kRows);
+      ml[u] = make_float2(kNone, 0.f), x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (kk <= c1) {
+        x[u] = __ldcg(reinterpret_cast<const float4 *>(from + row * kHd + ch));
+        ml[u] = __ldcg(reinterpret_cast<const float2 *>(from + kRows * kHd + 2 * row));
+      }
+    }
+    float mm = m;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) mm = fmaxf(mm, ml[u].x);
+    float f = ex2(m - mm);
+    a = make_float4(a.x * f, a.y * f, a.z * f, a.w * f), l *= f, m = mm;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      f = ex2(ml[u].x - m);
+      a.x = __fmaf_rn(x[u].x, f, a.x), a.y = __fmaf_rn(x[u].y, f, a.y), a.z = __fmaf_rn(x[u].z, f, a.z), a.w = __fmaf_rn(x[u].w, f, a.w);
+      l = __fmaf_rn(ml[u].y, f, l);
+    }
+  }
+}
+
 // Tiles that other CTAs hold parts of too: one that began before this share, one that is left to the next ones (`tiles`, shared memory).  The CTA has stored its partial tiles; the
 // CTA that arrives last joins all of them, in the order of the shares: no CTA waits for another, and the bits are the same every time.  Threads 0 ... kThreads - 1, named barrier 1;
 // `span`: four ints, `scratch`: 32 bytes per thread of shared memory.
 template <int kHd, int kRows, int kTokens, int kThreads>
 __device__ __forceinline__ void join_shares(const AtParams &p, const Shares &shares, long long begin, const OpenTile *tiles, int *span, float4 *scratch) {
-  constexpr int kFloats = at_partial(kHd, kRows);
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   if (tiles[0].from == kNoTile && tiles[1].from == kNoTile) return;
   const bool mine = warp < 2 && lane == 0 && tiles[warp].from != kNoTile;
@@ -269,32 +299,7 @@ __device__ __forceinline__ void join_shares(const AtParams &p, const Shares &sha
       const int item = i % items, row = item / (kHd / 4), ch = 4 * (item % (kHd / 4));
       float m = kNone, l = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      constexpr int kAhead = 8;                      // loads in flight
-      for (int k = c0 + i / items; k <= c1; k += kAhead * split) {
-        float4 x[kAhead];
-        float2 ml[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int kk = k + u * split;
-          const float *const from = p.partials + (2ll * kk + (kk == c0)) * kFloats;
-          ml[u] = make_float2(kNone, 0.f), x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (kk <= c1) {
-            x[u] = __ldcg(reinterpret_cast<const float4 *>(from + row * kHd + ch));
-            ml[u] = __ldcg(reinterpret_cast<const float2 *>(from + kRows * kHd + 2 * row));
-          }
-        }
-        float mm = m;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) mm = fmaxf(mm, ml[u].x);
-        float f = ex2(m - mm);
-        a = make_float4(a.x * f, a.y * f, a.z * f, a.w * f), l *= f, m = mm;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          f = ex2(ml[u].x - m);
-          a.x = __fmaf_rn(x[u].x, f, a.x), a.y = __fmaf_rn(x[u].y, f, a.y), a.z = __fmaf_rn(x[u].z, f, a.z), a.w = __fmaf_rn(x[u].w, f, a.w);
-          l = __fmaf_rn(ml[u].y, f, l);
-        }
-      }
+      gather<kHd, kRows>(p, row, ch, c0, c1, c0 + i / items, split, a, m, l);
       if (split == 1) store_row4<kHd>(p, row_at<kHd>(p, s.row, head, first_row + row), ch, a, m, l);
       else scratch[2 * i] = a, scratch[2 * i + 1] = make_float4(m, l, 0.f, 0.f);
     }

@@ -1,7 +1,7 @@
 // rosaq_attend for many query rows per sequence and key/value head: a prompt, or a batch behind a shared prefix.
 //
 // Bound: the tensor core, so it is tcgen05 here: per chunk of 64 tokens S = Q K^T (128 rows x 64 tokens, both operands in shared memory) and O += P V (P in tensor memory over its
-// scores, V in shared memory), fp32 accumulators in tensor memory.  A CTA has up to two tiles of 128 rows, which share every key and value that four warps make of the codes:
+// scores, V in shared memory), fp32 accumulators in tensor memory.  A CTA has up to two tiles of 128 rows, which share every key and value that eight warps make of the codes:
 // lo + scale * code in one fp16 fused multiply-add, i.e. rounded once to fp16 (2^-11; as are the softmax weights), in the fragment order of the cache's words, so that one stmatrix
 // stores four 8 x 8 pieces: rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  While the tensor core
 // works on one tile's chunk, four warps do the softmax of the other's, a row per thread; the scores of the next chunk go to a second buffer.  The maximum of a row is renewed only
@@ -18,8 +18,16 @@ namespace {
 constexpr int kTile = 128, kRows = 2 * kTile;       // query rows of an MMA, of a CTA's tile
 constexpr int kTokens = 64, kBlocks = kTokens / kKvBlock;
 constexpr int kWorkers = 8;                         // softmax warps
-constexpr int kConsumers = 32 * kWorkers, kMakers = 4;
+constexpr int kMakers = 8;                           // four of keys, four of values
 constexpr int kThreads = 32 * (kWorkers + kMakers + 2);
+constexpr int kFew = 16, kLeast = 4;                // chunks: of tiles that are not cut, of a CTA
+constexpr int kJoinRows = 16, kJoinThreads = 256;
+
+// A tile that begins in a CTA's share and does not end there, for the launch that joins the parts: behind the partial tiles of all CTAs, one per CTA.
+struct OpenRows {
+  int rows;             // 0: there is none
+  int head, first_row, seq_row, last_cta, pad[3];
+};
 
 template <int kHd, int kBits>
 struct RCfg {
@@ -27,12 +35,14 @@ struct RCfg {
   static constexpr int kQBytes = kTile * 2 * kHd, kKBytes = kTokens * 2 * kHd, kVBytes = kKBytes;
   static constexpr int kRawBytes = kBlocks * kv_block_bytes(kHd, kBits);
   static constexpr int kRaw = 3;                    // chunks of codes under way
-  static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + 2 * kKBytes, kOffRaw = kOffV + 2 * kVBytes, kOffBars = kOffRaw + kRaw * kRawBytes;
+  static constexpr int kKv = (226 * 1024 - 2048 - 2 * kQBytes - kRaw * kRawBytes) / (2 * kKBytes) < 4 ? 3 : 4;   // chunks of keys and values: with two, the makers wait for the tensor core and it for them
+  static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + kKv * kKBytes, kOffRaw = kOffV + kKv * kVBytes, kOffBars = kOffRaw + kRaw * kRawBytes;
   static constexpr int kSmem = kOffBars + 512 + 1024;   // (the swizzled operands start at a multiple of 1024)
-  static constexpr long long kWorkBytes = 2 * 4 * at_partial(kHd, kRows);   // of a CTA
+  static constexpr long long kWorkBytes = 2 * 4 * at_partial(kHd, kRows) + (int)sizeof(OpenRows);   // of a CTA
 };
 // barriers
-constexpr int kRawFull = 0, kRawEmpty = 4, kKvFull = 8, kKFree = 10, kVFree = 12, kSFull = 14 /* [tile][buffer] */, kPFull = 18, kODone = 22 /* [tile] */, kQFull = 24, kDone = 26, kBars = 27;
+constexpr int kRawFull = 0, kRawEmpty = 4, kKFull = 8, kVFull = 12, kKFree = 16, kVFree = 20, kSFull = 24 /* [tile][buffer] */, kPFull = 28, kODone = 32 /* [tile] */, kQFull = 34, kDone = 36,
+              kBars = 37;
 // tensor memory
 __device__ __forceinline__ uint32_t s_col(int tile, int buf) { return 128 * tile + 64 * buf; }
 __device__ __forceinline__ uint32_t o_col(int tile) { return 256 + 128 * tile; }
@@ -92,27 +102,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   extern __shared__ uint8_t dyn[];
   uint8_t *const smem = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
   const uint32_t base = smem_u32(smem), bars = base + C::kOffBars;
-  OpenTile *const open = reinterpret_cast<OpenTile *>(smem + C::kOffBars + 8 * kBars);   // [2] tiles that other CTAs hold parts of too
-  int *const span = reinterpret_cast<int *>(open + 2);
-  uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(span + 4);
+  uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(smem + C::kOffBars + 8 * kBars);
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return bars + 8 * i; };
 
   Share share;
-  if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, 16, 4, blockIdx.x == 0 && warp == 0, share)) return;
+  OpenRows *const open = reinterpret_cast<OpenRows *>(p.partials + 2ll * gridDim.x * at_partial(kHd, kRows)) + blockIdx.x;
+  if (threadIdx.x == 0) open->rows = 0;
+  if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, kFew, kLeast, blockIdx.x == 0 && warp == 0, share)) return;
   Cursor cur = share.cur;
   const int n = (int)(share.end - share.begin);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kRaw; ++i) mbar_init(bar(kRawFull + i), 1), mbar_init(bar(kRawEmpty + i), kMakers);
+    for (int i = 0; i < C::kKv; ++i) mbar_init(bar(kKFull + i), 4), mbar_init(bar(kVFull + i), 4), mbar_init(bar(kKFree + i), 1), mbar_init(bar(kVFree + i), 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(kKvFull + i), kMakers), mbar_init(bar(kKFree + i), 1), mbar_init(bar(kVFree + i), 1);
       mbar_init(bar(kODone + i), 1), mbar_init(bar(kQFull + i), 4);
       for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4);
     }
     mbar_init(bar(kDone), 1);
     mbar_init_fence();
-    open[0].from = open[1].from = kNoTile;
   }
   if (warp == kWorkers + kMakers) tmem_alloc<512>(smem_u32(tmem_at));
   tc_fence_before();
@@ -150,15 +159,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       if (active && sg.count > 0) {
         // ---- the queries
         const __half *const src = p.q + (long long)(s.row + tok) * p.ldq + (long long)(sg.head * p.group + (valid ? flat - tok * p.group : 0)) * kHd;
-        uint8_t *const q = smem + x * C::kQBytes + 128 * row;
+        // (kLanes lanes per row, so that a row's bytes are read together)
+        constexpr int kLanes = kHd / 8, kPer = 32 / kLanes;
+        const int piece = lane % kLanes;
 #pragma unroll
-        for (int k = 0; k < kHd / 8; ++k) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (valid) v = *reinterpret_cast<const uint4 *>(src + 8 * k);
-          __half2 *const h = reinterpret_cast<__half2 *>(&v);
+        for (int i0 = 0; i0 < 32 / kPer; i0 += 8) {
+          uint4 v[8];                                // (all loads before the first store, which might be to their memory for all the compiler knows)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = __hmul2(h[e], sign);
-          *reinterpret_cast<uint4 *>(q + (k / 8) * (128 * kTile) + (((k & 7) ^ (row & 7)) << 4)) = v;
+          for (int i = 0; i < 8; ++i) {
+            const int of = kPer * (i0 + i) + lane / kLanes;
+            const __half *const from = reinterpret_cast<const __half *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), of));
+            const bool there = __shfl_sync(0xffffffffu, valid, of);
+            v[i] = there ? *reinterpret_cast<const uint4 *>(from + 8 * piece) : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int to = 32 * (warp & 3) + kPer * (i0 + i) + lane / kLanes;
+            __half2 *const h = reinterpret_cast<__half2 *>(&v[i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = __hmul2(h[e], sign);
+            *reinterpret_cast<uint4 *>(smem + x * C::kQBytes + (piece / 8) * (128 * kTile) + 128 * to + (((piece & 7) ^ (to & 7)) << 4)) = v[i];
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -170,22 +191,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           bool through = j == 0;                     // the product before this one is
           wait(kSFull + 2 * x + buf, (g >> 1) & 1);
           tc_fence_after();
-          float sc[kTokens];
+          // The scores are read twice, 32 at a time, rather than held: registers for the makers' warps.
+          const bool border = tok0 + kTokens > least;
+          auto scores = [&](int half, float *sc) {
+            tmem_ld16(lanes + s_col(x, buf) + 32 * half, reinterpret_cast<uint32_t *>(sc));
+            tmem_ld16(lanes + s_col(x, buf) + 32 * half + 16, reinterpret_cast<uint32_t *>(sc + 16));
+            tc_wait_ld();
+            if (border) {
 #pragma unroll
-          for (int i = 0; i < kTokens / 16; ++i) tmem_ld16(lanes + s_col(x, buf) + 16 * i, reinterpret_cast<uint32_t *>(sc + 16 * i));
-          tc_wait_ld();
-          if (tok0 + kTokens > least) {
+              for (int i = 0; i < 32; ++i)
+                if (tok0 + 32 * half + i >= lim) sc[i] = -INFINITY;
+            }
+          };
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < kTokens; ++i)
-              if (tok0 + i >= lim) sc[i] = -INFINITY;
+          for (int half = 0; half < 2; ++half) {
+            float sc[32];
+            scores(half, sc);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], sc[i]);
           }
-          float m[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) m[i] = fmaxf(sc[i], sc[i + 4]);
-#pragma unroll
-          for (int i = 8; i < kTokens; i += 4)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m[e] = fmaxf(m[e], sc[i + e]);
           const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a;
           if (__any_sync(0xffffffffu, most > top + kGrow)) {
             const float now = fmaxf(most, top), f = ex2(top - now);
@@ -205,17 +230,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             }
           }
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t w[kTokens / 2];
 #pragma unroll
-          for (int i = 0; i < kTokens / 2; ++i) {
-            const float u = ex2(__fmaf_rn(sc[2 * i], a, -top)), v = ex2(__fmaf_rn(sc[2 * i + 1], a, -top));
-            sum[2 * (i & 1)] += u, sum[2 * (i & 1) + 1] += v;
-            w[i] = pack_h2(u, v);
+          for (int half = 0; half < 2; ++half) {
+            float sc[32];
+            scores(half, sc);
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float u = ex2(__fmaf_rn(sc[2 * i], a, -top)), v = ex2(__fmaf_rn(sc[2 * i + 1], a, -top));
+              sum[2 * (i & 1)] += u, sum[2 * (i & 1) + 1] += v;
+              w[i] = pack_h2(u, v);
+            }
+            // the weights over scores that have been read: sixteen columns hold 32 of them
+            tmem_st16(lanes + s_col(x, buf) + 16 * half, w);
           }
           den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          // the weights over the first half of the scores
-          tmem_st16(lanes + s_col(x, buf), w);
-          tmem_st16(lanes + s_col(x, buf) + 16, w + 16);
           tc_wait_st();
           // (every phase of that barrier is waited for, before the next one can end)
           if (!through) wait(kODone + x, (g - 1) & 1);
@@ -229,38 +258,75 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       // ---- the rows, or this CTA's part of them
       const int from = n - left - sg.chunk0;
       if (active) {
+        // By way of shared memory (the place of this warp's queries), 32 channels at a time, so that eight lanes write to a row: a row per lane takes 32 sectors per
+        // instruction (a tile of one chunk 20.2 us that way).
         const int r = kTile * x + row;
-        float *const part = my_partial(p, from, at_partial(kHd, kRows));
         const RowAt to = row_at<kHd>(p, s.row, sg.head, valid ? flat : 0);
+        float *const sums = !sg.whole ? my_partial(p, from, at_partial(kHd, kRows)) + r * kHd : to.prefix;   // where a part, or a prefix launch's result, goes
+        const bool finish = sg.whole && p.prefix_tokens == 0;
+        float f = 1.f, g = 0.f;
+        if (finish) {
+          float l = den;
+          if (to.prefix && valid) {
+            const float2 ml = *reinterpret_cast<const float2 *>(to.prefix + kHd);
+            const float mm = fmaxf(top, ml.x);
+            f = ex2(top - mm), g = ex2(ml.x - mm), l = l * f + ml.y * g;
+          }
+          const float inv = l == 0.f ? 0.f : 1.f / l;   // no token: zeros
+          f *= inv, g *= inv;
+        } else if (valid) {
+          float *const at = sg.whole ? to.prefix + kHd : sums - r * kHd + kRows * kHd + 2 * r;
+          *reinterpret_cast<float2 *>(at) = make_float2(top, den);
+        }
+        uint8_t *const stage = smem + x * C::kQBytes + 4096 * (warp & 3);
 #pragma unroll 1
-        for (int i = 0; i < kHd; i += 16) {
-          float o[16];
+        for (int ch = 0; ch < kHd; ch += 32) {
+          float o[32];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = 0.f;
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
           if (sg.count > 0) {
-            tmem_ld16(lanes + o_col(x) + i, reinterpret_cast<uint32_t *>(o));
+            tmem_ld16(lanes + o_col(x) + ch, reinterpret_cast<uint32_t *>(o));
+            tmem_ld16(lanes + o_col(x) + ch + 16, reinterpret_cast<uint32_t *>(o + 16));
             tc_wait_ld();
           }
-          if (!valid) continue;
+          __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const float4 v = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            if (sg.whole) store_row4<kHd>(p, to, i + e, v, top, den);
-            else *reinterpret_cast<float4 *>(part + r * kHd + i + e) = v;
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4 *>(stage + 128 * lane + (((e / 4) ^ (lane & 7)) << 4)) = make_float4(o[e] * f, o[e + 1] * f, o[e + 2] * f, o[e + 3] * f);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int of = 4 * i + lane / 8, at = ch + 4 * (lane & 7);
+            float4 v = *reinterpret_cast<const float4 *>(stage + 128 * of + (((lane & 7) ^ (of & 7)) << 4));
+            const bool there = __shfl_sync(0xffffffffu, valid, of);
+            float *const to_sums = reinterpret_cast<float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(sums), of));
+            __half *const to_out = reinterpret_cast<__half *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to.out), of));
+            const float gg = __shfl_sync(0xffffffffu, g, of);
+            if (!there) continue;
+            if (finish) {
+              if (p.prefix) {
+                const float4 w = *reinterpret_cast<const float4 *>(to_sums + at);
+                v = make_float4(__fmaf_rn(w.x, gg, v.x), __fmaf_rn(w.y, gg, v.y), __fmaf_rn(w.z, gg, v.z), __fmaf_rn(w.w, gg, v.w));
+              }
+              uint2 h;
+              h.x = pack_h2(v.x, v.y), h.y = pack_h2(v.z, v.w);
+              *reinterpret_cast<uint2 *>(to_out + at) = h;
+            } else {
+              *reinterpret_cast<float4 *>(to_sums + at) = v;
+            }
           }
         }
-        if (valid && !sg.whole) *reinterpret_cast<float2 *>(part + kRows * kHd + 2 * r) = make_float2(top, den);
       }
-      if (!sg.whole && threadIdx.x == 0) open[from < 0 ? 0 : 1] = OpenTile{from, cur.seq, cur.unit, s.chunks};
+      if (threadIdx.x == 0 && from >= 0 && from + s.chunks > n) {
+        open->head = sg.head, open->first_row = sg.tile * kRows, open->seq_row = s.row, open->rows = sg.rows;
+        open->last_cta = share.all.last(share.begin + from, s.chunks);
+      }
       tc_fence_before();
       left -= take, cur.chunk += take;
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(kConsumers) : "memory");
-    // (the queries are not needed any more)
-    join_shares<kHd, kRows, kTokens, kConsumers>(p, share.all, share.begin, open, span, reinterpret_cast<float4 *>(smem));
   } else if (warp < kWorkers + kMakers) {
-    // ================================================================ keys and values from codes: a block of sixteen tokens per warp
-    const int blk = warp - kWorkers, r = lane >> 2, c = lane & 3;
+    // ================================================================ keys or values from codes: a block of sixteen tokens per warp
+    const int blk = (warp - kWorkers) & 3, value = (warp - kWorkers) >> 2, r = lane >> 2, c = lane & 3;
     // where stmatrix puts the four pieces of a step: this lane names row lane & 7 of piece lane >> 3
     const int h1 = (lane >> 3) & 1, h2 = lane >> 4;
     uint32_t g = 0;
@@ -269,11 +335,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       const Segment sg = segment(p, cur, left);
       const int take = min(left, cur.s.chunks - cur.chunk);
       for (int j = 0; j < sg.count; ++j, ++g) {
-        const int st = g & 1, raw = g % C::kRaw;
+        const int st = g % C::kKv, raw = g % C::kRaw;
         const uint32_t from = base + C::kOffRaw + raw * C::kRawBytes + blk * kBlockBytes;
         const int tok0 = (sg.chunk0 + j) * kTokens + blk * kKvBlock;
         wait(kRawFull + raw, (g / C::kRaw) & 1);
-        if (g >= 2) wait(kKFree + st, (g / 2 - 1) & 1), wait(kVFree + st, (g / 2 - 1) & 1);
+        if (g >= (uint32_t)C::kKv) wait((value ? kVFree : kKFree) + st, (g / C::kKv - 1) & 1);
         // scale and least value; zeros behind the last token, whatever lies there.  (A group that reaches to the end of fp16 may pass it with its greatest code: the
         // scale is a step smaller then.)
         auto pair = [&](uint32_t at, int tok) {
@@ -283,8 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           return tok < cur.s.len ? v : 0u;
         };
         constexpr int kPairs = 2 * kv_code_bytes(kHd, kBits);
-#pragma unroll
-        for (int value = 0; value < 2; ++value) {
+        {
           uint32_t sc[2], lo[2];                     // keys: of tokens r and r + 8, twice each; values: of tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -325,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kKvFull + st)), mbar_arrive(bar(kRawEmpty + raw));
+        if (lane == 0) mbar_arrive(bar((value ? kVFull : kKFull) + st)), mbar_arrive(bar(kRawEmpty + raw));
       }
       left -= take, cur.chunk += take;
     }
@@ -339,7 +404,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       const int take = min(left, cur.s.chunks - cur.chunk), tiles = sg.rows > kTile ? 2 : 1;
       auto scores = [&](int j) {                     // of chunk j of the segment
         const uint32_t at = g + j;
-        wait(kKvFull + (at & 1), (at >> 1) & 1);
+        const uint32_t st = at % C::kKv;
+        wait(kKFull + st, (at / C::kKv) & 1);
         tc_fence_after();
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -348,28 +414,29 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           if (!lost)
 #pragma unroll
             for (int h = 0; h < C::kHalves; ++h)
-              mma4_ss(tmem + s_col(x, gj & 1), make_b_desc(base + x * C::kQBytes + h * 128 * kTile), make_b_desc(base + C::kOffK + (at & 1) * C::kKBytes + h * 128 * kTokens),
+              mma4_ss(tmem + s_col(x, gj & 1), make_b_desc(base + x * C::kQBytes + h * 128 * kTile), make_b_desc(base + C::kOffK + st * C::kKBytes + h * 128 * kTokens),
                       idesc_s, h);
           tc_commit(bar(kSFull + 2 * x + (gj & 1)));
         }
-        tc_commit(bar(kKFree + (at & 1)));
+        tc_commit(bar(kKFree + st));
       };
       if (sg.count > 0) {
         for (int x = 0; x < tiles; ++x) wait(kQFull + x, segs[x]++ & 1);
         scores(0);
         for (int j = 0; j < sg.count; ++j) {
           if (j + 1 < sg.count) scores(j + 1);
-          const uint32_t at = g + j;
+          const uint32_t at = g + j, st = at % C::kKv;
+          wait(kVFull + st, (at / C::kKv) & 1);
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (x >= tiles) continue;
             const uint32_t gj = gx[x] + j;
             wait(kPFull + 2 * x + (gj & 1), (gj >> 1) & 1);
             tc_fence_after();
-            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, gj & 1), make_b_desc(base + C::kOffV + (at & 1) * C::kVBytes), idesc_o, j > 0);
+            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, gj & 1), make_b_desc(base + C::kOffV + st * C::kVBytes), idesc_o, j > 0);
             tc_commit(bar(kODone + x));
           }
-          tc_commit(bar(kVFree + (at & 1)));
+          tc_commit(bar(kVFree + st));
         }
         g += sg.count, gx[0] += sg.count;
         if (tiles == 2) gx[1] += sg.count;
@@ -414,10 +481,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   if (warp == kWorkers + kMakers) tmem_dealloc<512>(tmem);
 }
 
+// The parts of tiles that several CTAs hold, in the order of the list: kJoinRows rows of the tile that begins in share blockIdx.x and does not end there.  (One CTA that arrives last
+// would have 135 KB per part to read: behind a prefix of 16001 tokens, 18 parts of 256 rows, 220 us in all.)
+template <int kHd>
+__global__ void __launch_bounds__(kJoinThreads) attend_rows_join_kernel(const __grid_constant__ AtParams p, int ctas) {
+  grid_dep_launch_dependents();
+  grid_dep_wait();
+  const OpenRows open = reinterpret_cast<const OpenRows *>(p.partials + 2ll * ctas * at_partial(kHd, kRows))[blockIdx.x];
+  const int c0 = blockIdx.x;
+  for (int i = threadIdx.x; i < kJoinRows * (kHd / 4); i += kJoinThreads) {
+    const int row = blockIdx.y * kJoinRows + i / (kHd / 4), ch = 4 * (i % (kHd / 4));
+    if (row >= open.rows) break;
+    float m = kNone, l = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    gather<kHd, kRows>(p, row, ch, c0, open.last_cta, c0, 1, a, m, l);
+    store_row4<kHd>(p, row_at<kHd>(p, open.seq_row, open.head, open.first_row + row), ch, a, m, l);
+  }
+}
+
 template <int kHd, int kBits>
 int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   using C = RCfg<kHd, kBits>;
-  static_assert(C::kSmem <= 227 * 1024 && 8 * kBars + 2 * sizeof(OpenTile) + 32 <= 512 && 32 * kConsumers <= 2 * C::kQBytes, "shared memory");
+  static_assert(C::kSmem <= 227 * 1024 && 8 * kBars + 16 <= 512, "shared memory");
   auto *const kern = attend_rows_kernel<kHd, kBits>;
   int &ready = ctx->at_per_sm[4 + (kHd == 64) + 2 * (kBits == 8)];
   if (ready == 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
@@ -432,7 +517,7 @@ int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   // Not chained to the launch before it: a CTA takes all of an SM's tensor memory, which a CTA of that launch may still be going to ask for.
   kern<<<ctas, kThreads, C::kSmem, s>>>(p);
   if (cudaGetLastError() != cudaSuccess) return ROSAQ_ERR_CUDA;
-  return ROSAQ_OK;
+  return kv_launch(attend_rows_join_kernel<kHd>, dim3(ctas, kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
 }
 
 }  // namespace
