@@ -34,15 +34,15 @@ struct RCfg {
   static constexpr int kHalves = kHd / 64;          // 64 channels: a row of 128 bytes
   static constexpr int kQBytes = kTile * 2 * kHd, kKBytes = kTokens * 2 * kHd, kVBytes = kKBytes;
   static constexpr int kRawBytes = kBlocks * kv_block_bytes(kHd, kBits);
-  static constexpr int kRaw = 3;                    // chunks of codes under way
-  static constexpr int kKv = (226 * 1024 - 2048 - 2 * kQBytes - kRaw * kRawBytes) / (2 * kKBytes) < 4 ? 3 : 4;   // chunks of keys and values: with two, the makers wait for the tensor core and it for them
+  static constexpr int kRaw = kBits == 4 ? 6 : kHd == 64 ? 4 : 3;   // chunks of codes under way: three of 8.7 KB do not cover the latency of the memory
+  static constexpr int kKv = 3;                     // chunks of keys and values: with two, the makers wait for the tensor core and it for them
   static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + kKv * kKBytes, kOffRaw = kOffV + kKv * kVBytes, kOffBars = kOffRaw + kRaw * kRawBytes;
   static constexpr int kSmem = kOffBars + 512 + 1024;   // (the swizzled operands start at a multiple of 1024)
   static constexpr long long kWorkBytes = 2 * 4 * at_partial(kHd, kRows) + (int)sizeof(OpenRows);   // of a CTA
 };
 // barriers
-constexpr int kRawFull = 0, kRawEmpty = 4, kKFull = 8, kVFull = 12, kKFree = 16, kVFree = 20, kSFull = 24 /* [tile][buffer] */, kPFull = 28, kODone = 32 /* [tile] */, kQFull = 34, kDone = 36,
-              kBars = 37;
+constexpr int kRawFull = 0, kRawEmpty = 6, kKFull = 12, kVFull = 15, kKFree = 18, kVFree = 21, kSFull = 24 /* [tile][buffer] */, kPFull = 28, kODone = 32 /* [tile][buffer] */, kQFull = 36,
+              kDone = 38, kBars = 39;
 // tensor memory
 __device__ __forceinline__ uint32_t s_col(int tile, int buf) { return 128 * tile + 64 * buf; }
 __device__ __forceinline__ uint32_t o_col(int tile) { return 256 + 128 * tile; }
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   uint8_t *const smem = dyn + ((1024 - (smem_u32(dyn) & 1023)) & 1023);
   const uint32_t base = smem_u32(smem), bars = base + C::kOffBars;
   uint32_t *const tmem_at = reinterpret_cast<uint32_t *>(smem + C::kOffBars + 8 * kBars);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   auto bar = [&](int i) { return bars + 8 * i; };
 
   Share share;
@@ -117,8 +117,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     for (int i = 0; i < C::kRaw; ++i) mbar_init(bar(kRawFull + i), 1), mbar_init(bar(kRawEmpty + i), kMakers);
     for (int i = 0; i < C::kKv; ++i) mbar_init(bar(kKFull + i), 4), mbar_init(bar(kVFull + i), 4), mbar_init(bar(kKFree + i), 1), mbar_init(bar(kVFree + i), 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(kODone + i), 1), mbar_init(bar(kQFull + i), 4);
-      for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4);
+      mbar_init(bar(kQFull + i), 4);
+      for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4), mbar_init(bar(kODone + 2 * i + b), 1);
     }
     mbar_init(bar(kDone), 1);
     mbar_init_fence();
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_at;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
 
   // A wait that expires is reported, and the warp waits no more: it goes on through what the others rely on.
   bool lost = false;
@@ -141,6 +141,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     }
   };
 
+  // The same without the suspension of mbarrier.try_wait, which takes its time to end: for the one warp that everybody waits for.
+  auto spin = [&](int b, uint32_t parity) {
+    if (lost) return;
+    bool here = mbar_test_wait(bar(b), parity);
+    if (__all_sync(0xffffffffu, here)) return;
+    for (long long i = 0; !here && i < 32 * p.wait_limit; ++i) here = mbar_test_wait(bar(b), parity);
+    lost = !__all_sync(0xffffffffu, here);
+    if (lost && lane == 0) atomicExch(p.status, (int)ROSAQ_ERR_TIMEOUT);
+  };
+
   if (warp < kWorkers) {
     // ================================================================ softmax: warps 0-3 the first tile, 4-7 the second; a row per thread
     const int x = warp >> 2, row = 32 * (warp & 3) + lane;
@@ -148,6 +158,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     const float a = fmaxf(fabsf(p.scale_log2), 1e-30f);   // (its sign is in the queries)
     const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : p.scale_log2 == 0.f ? 0.f : 1.f);
     uint32_t g = 0;                                  // chunks of this tile so far
+    // The products of chunk k and all before it are through.  Every phase of the two barriers is waited for, in order and before the next one of the same barrier can end.
+    uint32_t through = 0;
+    auto product = [&](uint32_t chunks) {
+      for (; through < chunks; ++through) wait(kODone + 2 * x + (through & 1), (through >> 1) & 1);
+    };
     for (int left = n; left > 0;) {
       settle<kRows, kTokens>(p, cur);
       const Segment sg = segment(p, cur, left);
@@ -188,15 +203,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         const int least = __reduce_min_sync(0xffffffffu, lim);
         for (int j = 0; j < sg.count; ++j, ++g) {
           const int buf = g & 1, tok0 = (sg.chunk0 + j) * kTokens;
-          bool through = j == 0;                     // the product before this one is
           wait(kSFull + 2 * x + buf, (g >> 1) & 1);
           tc_fence_after();
-          // The scores are read twice, 32 at a time, rather than held: registers for the makers' warps.
+          // The scores are read twice rather than held: registers for the makers' warps.
           const bool border = tok0 + kTokens > least;
-          auto scores = [&](int half, float *sc) {
+          auto load = [&](int half, float *sc) {
             tmem_ld16(lanes + s_col(x, buf) + 32 * half, reinterpret_cast<uint32_t *>(sc));
             tmem_ld16(lanes + s_col(x, buf) + 32 * half + 16, reinterpret_cast<uint32_t *>(sc + 16));
-            tc_wait_ld();
+          };
+          auto mask = [&](int half, float *sc) {
             if (border) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
@@ -204,19 +219,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             }
           };
           float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float s0[32], s1[32];
+          load(0, s0), load(1, s1);
+          tc_wait_ld();
+          mask(0, s0), mask(1, s1);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float sc[32];
-            scores(half, sc);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], sc[i]);
-          }
+          for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], fmaxf(s0[i], s1[i]));
           const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a;
           if (__any_sync(0xffffffffu, most > top + kGrow)) {
             const float now = fmaxf(most, top), f = ex2(top - now);
             top = now, den *= f;
             if (j > 0) {
-              wait(kODone + x, (g - 1) & 1), through = true;
+              product(g);
               tc_fence_after();
 #pragma unroll 1
               for (int i = 0; i < kHd; i += 16) {
@@ -230,10 +244,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             }
           }
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float sc[32];
-            scores(half, sc);
+          load(1, s1);                               // (on its way under the first half's exponentials)
+          auto weigh = [&](int half, const float *sc) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -243,16 +255,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             }
             // the weights over scores that have been read: sixteen columns hold 32 of them
             tmem_st16(lanes + s_col(x, buf) + 16 * half, w);
-          }
+          };
+          weigh(0, s0);
+          tc_wait_ld();
+          mask(1, s1);
+          weigh(1, s1);
           den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tc_wait_st();
-          // (every phase of that barrier is waited for, before the next one can end)
-          if (!through) wait(kODone + x, (g - 1) & 1);
+          if (g > 0) product(g - 1);                 // (not the last one's: that would have it in line with this softmax)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(kPFull + 2 * x + buf));
         }
-        wait(kODone + x, (g - 1) & 1);
+        product(g);
         tc_fence_after();
       }
       // ---- the rows, or this CTA's part of them
@@ -395,51 +410,69 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       left -= take, cur.chunk += take;
     }
   } else if (warp == kWorkers + kMakers) {
-    // ================================================================ MMAs
-    const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
-    uint32_t g = 0, gx[2] = {0, 0}, segs[2] = {0, 0};
+    // ================================================================ MMAs.  Everything that addresses them is the same in all lanes, and the compiler can see it (what came
+    // from memory by way of a shuffle): it then lies in uniform registers, and an MMA is issued in its own time instead of 60 cycles.
+    constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
+    const uint32_t ubase = __shfl_sync(0xffffffffu, base, 0), ubars = ubase + C::kOffBars;
+    const uint64_t q_desc = make_b_desc(ubase), k_desc = make_b_desc(ubase + C::kOffK), v_desc = make_b_desc(ubase + C::kOffV);
+    constexpr uint32_t kQ16 = C::kQBytes / 16, kQHalf16 = 8 * kTile, kK16 = C::kKBytes / 16, kKHalf16 = 8 * kTokens, kV16 = C::kVBytes / 16;
+    auto ubar = [&](int i) { return ubars + 8 * i; };
+    int k_at = 0, v_at = 0;                          // slots of the next keys and values ...
+    uint32_t k_turn = 0, v_turn = 0;                 // ... and the parity of their barriers
+    uint32_t score0 = 0, score1 = 0, weigh0 = 0, weigh1 = 0, segs0 = 0, segs1 = 0;   // chunks of each tile whose scores, whose products have been issued; tiles of queries
+    // scores of the next chunk
+    auto scores = [&](bool two) {
+      spin(kKFull + k_at, k_turn);
+      tc_fence_after();
+      const uint64_t k = k_desc + (uint64_t)(k_at * kK16);
+      if (!lost) {
+#pragma unroll
+        for (int h = 0; h < C::kHalves; ++h)
+          mma4_ss(tmem + s_col(0, score0 & 1), q_desc + h * kQHalf16, k + h * kKHalf16, idesc_s, h);
+      }
+      tc_commit(ubar(kSFull + (score0 & 1)));
+      ++score0;
+      if (two) {
+        if (!lost) {
+#pragma unroll
+          for (int h = 0; h < C::kHalves; ++h)
+            mma4_ss(tmem + s_col(1, score1 & 1), q_desc + kQ16 + h * kQHalf16, k + h * kKHalf16, idesc_s, h);
+        }
+        tc_commit(ubar(kSFull + 2 + (score1 & 1)));
+        ++score1;
+      }
+      tc_commit(ubar(kKFree + k_at));
+      if (++k_at == C::kKv) k_at = 0, k_turn ^= 1;
+    };
     for (int left = n; left > 0;) {
       settle<kRows, kTokens>(p, cur);
       const Segment sg = segment(p, cur, left);
-      const int take = min(left, cur.s.chunks - cur.chunk), tiles = sg.rows > kTile ? 2 : 1;
-      auto scores = [&](int j) {                     // of chunk j of the segment
-        const uint32_t at = g + j;
-        const uint32_t st = at % C::kKv;
-        wait(kKFull + st, (at / C::kKv) & 1);
-        tc_fence_after();
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (x >= tiles) continue;
-          const uint32_t gj = gx[x] + j;
-          if (!lost)
-#pragma unroll
-            for (int h = 0; h < C::kHalves; ++h)
-              mma4_ss(tmem + s_col(x, gj & 1), make_b_desc(base + x * C::kQBytes + h * 128 * kTile), make_b_desc(base + C::kOffK + st * C::kKBytes + h * 128 * kTokens),
-                      idesc_s, h);
-          tc_commit(bar(kSFull + 2 * x + (gj & 1)));
-        }
-        tc_commit(bar(kKFree + st));
-      };
-      if (sg.count > 0) {
-        for (int x = 0; x < tiles; ++x) wait(kQFull + x, segs[x]++ & 1);
-        scores(0);
-        for (int j = 0; j < sg.count; ++j) {
-          if (j + 1 < sg.count) scores(j + 1);
-          const uint32_t at = g + j, st = at % C::kKv;
-          wait(kVFull + st, (at / C::kKv) & 1);
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (x >= tiles) continue;
-            const uint32_t gj = gx[x] + j;
-            wait(kPFull + 2 * x + (gj & 1), (gj >> 1) & 1);
+      const int take = min(left, cur.s.chunks - cur.chunk);
+      const int count = __shfl_sync(0xffffffffu, sg.count, 0);
+      const bool two = __shfl_sync(0xffffffffu, sg.rows > kTile, 0);
+      if (count > 0) {
+        spin(kQFull, segs0++ & 1);
+        if (two) spin(kQFull + 1, segs1++ & 1);
+        scores(two);
+        for (int j = 0; j < count; ++j) {
+          if (j + 1 < count) scores(two);
+          spin(kVFull + v_at, v_turn);
+          const uint64_t v = v_desc + (uint64_t)(v_at * kV16);
+          spin(kPFull + (weigh0 & 1), (weigh0 >> 1) & 1);
+          tc_fence_after();
+          if (!lost) mma4_ts(tmem + o_col(0), tmem + s_col(0, weigh0 & 1), v, idesc_o, j > 0);
+          tc_commit(ubar(kODone + (weigh0 & 1)));
+          ++weigh0;
+          if (two) {
+            spin(kPFull + 2 + (weigh1 & 1), (weigh1 >> 1) & 1);
             tc_fence_after();
-            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, gj & 1), make_b_desc(base + C::kOffV + st * C::kVBytes), idesc_o, j > 0);
-            tc_commit(bar(kODone + x));
+            if (!lost) mma4_ts(tmem + o_col(1), tmem + s_col(1, weigh1 & 1), v, idesc_o, j > 0);
+            tc_commit(ubar(kODone + 2 + (weigh1 & 1)));
+            ++weigh1;
           }
-          tc_commit(bar(kVFree + st));
+          tc_commit(ubar(kVFree + v_at));
+          if (++v_at == C::kKv) v_at = 0, v_turn ^= 1;
         }
-        g += sg.count, gx[0] += sg.count;
-        if (tiles == 2) gx[1] += sg.count;
       }
       left -= take, cur.chunk += take;
     }
@@ -447,29 +480,33 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     tc_commit(bar(kDone));
     for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kDone), 0); ++i) {}
   } else {
-    // ================================================================ copies: lane i brings block i of the chunk
+    // ================================================================ copies: lane i brings block i of the chunk; its page is looked up a chunk ahead
     uint32_t g = 0;
     const uint64_t keep = policy_evict_first();
+    const int run = min(1 << p.kv.page_shift, kBlocks);   // blocks next to each other: one copy, by the lane of the first one
+    int block = 0, blocks = 0, page = 0;
+    const uint8_t *heads = nullptr;
+    auto look_up = [&](const Segment &sg, int j) {
+      block = (sg.chunk0 + j) * kBlocks, blocks = min(kBlocks, (cur.s.len + kKvBlock - 1) / kKvBlock - block);
+      heads = p.kv.pages + ((long long)sg.head << p.kv.page_shift) * kBlockBytes;
+      page = lane < blocks && lane % run == 0 ? kv_page(p.kv, p.b, cur.seq, block + lane) : 0;
+    };
     for (int left = n; left > 0;) {
       settle<kRows, kTokens>(p, cur);
       const Segment sg = segment(p, cur, left);
       const int take = min(left, cur.s.chunks - cur.chunk);
-      const uint8_t *const heads = p.kv.pages + ((long long)sg.head << p.kv.page_shift) * kBlockBytes;
+      if (sg.count > 0) look_up(sg, 0);
       for (int j = 0; j < sg.count && !lost; ++j, ++g) {
-        const int raw = g % C::kRaw, block = (sg.chunk0 + j) * kBlocks, blocks = min(kBlocks, (cur.s.len + kKvBlock - 1) / kKvBlock - block);
-        // runs of blocks of a page: one copy per run, by the lane of its first block
-        const int run = min(1 << p.kv.page_shift, kBlocks);
-        const bool mine = lane < blocks && lane % run == 0;
-        int page = 0;
-        if (mine) page = kv_page(p.kv, p.b, cur.seq, block + lane);
-        if (page < 0) kv_report(p.status), page = 0;         // (the first page of the cache in its place)
+        const int raw = g % C::kRaw;
         if (g >= (uint32_t)C::kRaw) wait(kRawEmpty + raw, (g / C::kRaw - 1) & 1);
         if (lost) break;
         if (lane == 0) mbar_arrive_expect_tx(bar(kRawFull + raw), blocks * kBlockBytes);
         __syncwarp();
-        if (mine)
+        if (page < 0) kv_report(p.status), page = 0;         // (the first page of the cache in its place)
+        if (lane < blocks && lane % run == 0)
           bulk_copy_g2s_hint(base + C::kOffRaw + raw * C::kRawBytes + lane * kBlockBytes, heads + kv_offset(p.kv, page, block + lane, kBlockBytes),
                              min(run, blocks - lane) * kBlockBytes, bar(kRawFull + raw), keep);
+        if (j + 1 < sg.count) look_up(sg, j + 1);
       }
       left -= take, cur.chunk += take;
     }
