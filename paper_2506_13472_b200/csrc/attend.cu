@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
   int *const span = reinterpret_cast<int *>(open + 2);
   // A warp's last part lies in its slots, which are free by then, an earlier one behind the partial tiles of all CTAs.
   uint8_t *const earlier = reinterpret_cast<uint8_t *>(p.partials + 2ll * gridDim.x * at_partial(kHd, kRows)) + (long long)blockIdx.x * 2 * kWarps * C::kPartBytes;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * C::kStages;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) mbar_init(full0 + 8 * i, 1), mbar_init(empty0 + 8 * i, 1);

@@ -19,7 +19,8 @@ constexpr int kTile = 128, kRows = 2 * kTile;       // query rows of an MMA, of 
 constexpr int kTokens = 64, kBlocks = kTokens / kKvBlock;
 constexpr int kWorkers = 8;                         // softmax warps
 constexpr int kMakers = 8;                           // four of keys, four of values
-constexpr int kThreads = 32 * (kWorkers + kMakers + 2);
+constexpr int kIssuers = kWorkers + kMakers;        // first of the two warps that issue MMAs, one per tile
+constexpr int kThreads = 32 * (kIssuers + 3);
 constexpr int kFew = 16, kLeast = 4;                // chunks: of tiles that are not cut, of a CTA
 constexpr int kJoinRows = 16, kJoinThreads = 256;
 
@@ -42,7 +43,7 @@ struct RCfg {
 };
 // barriers
 constexpr int kRawFull = 0, kRawEmpty = 6, kKFull = 12, kVFull = 15, kKFree = 18, kVFree = 21, kSFull = 24 /* [tile][buffer] */, kPFull = 28, kODone = 32 /* [tile][buffer] */, kQFull = 36,
-              kDone = 38, kBars = 39;
+              kDone = 38, kBars = 40;
 // tensor memory
 __device__ __forceinline__ uint32_t s_col(int tile, int buf) { return 128 * tile + 64 * buf; }
 __device__ __forceinline__ uint32_t o_col(int tile) { return 256 + 128 * tile; }
@@ -106,28 +107,31 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31;
   auto bar = [&](int i) { return bars + 8 * i; };
 
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kRaw; ++i) mbar_init(bar(kRawFull + i), 1), mbar_init(bar(kRawEmpty + i), kMakers);
+    for (int i = 0; i < C::kKv; ++i) mbar_init(bar(kKFull + i), 4), mbar_init(bar(kVFull + i), 4), mbar_init(bar(kKFree + i), 2), mbar_init(bar(kVFree + i), 2);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(kQFull + i), 4);
+      for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4), mbar_init(bar(kODone + 2 * i + b), 1);
+    }
+    mbar_init(bar(kDone), 1), mbar_init(bar(kDone + 1), 1);
+    mbar_init_fence();
+  }
+  // The launch before this one is over before the tensor memory is asked for, and those behind begin when this CTA has it: a CTA takes all that an SM has, and neither side may
+  // hold what the other one waits for.
+  grid_dep_wait();
   Share share;
   OpenRows *const open = reinterpret_cast<OpenRows *>(p.partials + 2ll * gridDim.x * at_partial(kHd, kRows)) + blockIdx.x;
   if (threadIdx.x == 0) open->rows = 0;
   if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, kFew, kLeast, blockIdx.x == 0 && warp == 0, share)) return;
   Cursor cur = share.cur;
   const int n = (int)(share.end - share.begin);
-
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < C::kRaw; ++i) mbar_init(bar(kRawFull + i), 1), mbar_init(bar(kRawEmpty + i), kMakers);
-    for (int i = 0; i < C::kKv; ++i) mbar_init(bar(kKFull + i), 4), mbar_init(bar(kVFull + i), 4), mbar_init(bar(kKFree + i), 1), mbar_init(bar(kVFree + i), 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(bar(kQFull + i), 4);
-      for (int b = 0; b < 2; ++b) mbar_init(bar(kSFull + 2 * i + b), 1), mbar_init(bar(kPFull + 2 * i + b), 4), mbar_init(bar(kODone + 2 * i + b), 1);
-    }
-    mbar_init(bar(kDone), 1);
-    mbar_init_fence();
-  }
-  if (warp == kWorkers + kMakers) tmem_alloc<512>(smem_u32(tmem_at));
+  if (warp == kIssuers) tmem_alloc<512>(smem_u32(tmem_at));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
+  grid_dep_launch_dependents();
 
   // A wait that expires is reported, and the warp waits no more: it goes on through what the others rely on.
   bool lost = false;
@@ -158,11 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     const float a = fmaxf(fabsf(p.scale_log2), 1e-30f);   // (its sign is in the queries)
     const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : p.scale_log2 == 0.f ? 0.f : 1.f);
     uint32_t g = 0;                                  // chunks of this tile so far
-    // The products of chunk k and all before it are through.  Every phase of the two barriers is waited for, in order and before the next one of the same barrier can end.
-    uint32_t through = 0;
-    auto product = [&](uint32_t chunks) {
-      for (; through < chunks; ++through) wait(kODone + 2 * x + (through & 1), (through >> 1) & 1);
-    };
+    // Products of chunk k end phase k / 2 of one of two barriers.  A phase is waited for only when the one before it on its barrier is known to have ended: chunk g waits for those
+    // of chunk g - 2, and those of chunk g - 1 only when it rescales.
     for (int left = n; left > 0;) {
       settle<kRows, kTokens>(p, cur);
       const Segment sg = segment(p, cur, left);
@@ -203,7 +204,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         const int least = __reduce_min_sync(0xffffffffu, lim);
         for (int j = 0; j < sg.count; ++j, ++g) {
           const int buf = g & 1, tok0 = (sg.chunk0 + j) * kTokens;
-          wait(kSFull + 2 * x + buf, (g >> 1) & 1);
+          // Scores of this chunk, and products of the last but one before it (which are older): both asked for at once, as an answer takes more than 100 cycles.
+          {
+            bool here = lost || mbar_try_wait(bar(kSFull + 2 * x + buf), (g >> 1) & 1), old = lost || g < 2 || mbar_try_wait(bar(kODone + 2 * x + buf), ((g >> 1) - 1) & 1);
+            if (!__all_sync(0xffffffffu, here && old)) {
+              wait(kSFull + 2 * x + buf, (g >> 1) & 1);
+              if (g >= 2) wait(kODone + 2 * x + buf, ((g >> 1) - 1) & 1);
+            }
+          }
           tc_fence_after();
           // The scores are read twice rather than held: registers for the makers' warps.
           const bool border = tok0 + kTokens > least;
@@ -230,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             const float now = fmaxf(most, top), f = ex2(top - now);
             top = now, den *= f;
             if (j > 0) {
-              product(g);
+              wait(kODone + 2 * x + (buf ^ 1), ((g - 1) >> 1) & 1);
               tc_fence_after();
 #pragma unroll 1
               for (int i = 0; i < kHd; i += 16) {
@@ -243,15 +251,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
               }
             }
           }
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 aa = make_float2(a, a), off = make_float2(-top, -top);
           load(1, s1);                               // (on its way under the first half's exponentials)
           auto weigh = [&](int half, const float *sc) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float u = ex2(__fmaf_rn(sc[2 * i], a, -top)), v = ex2(__fmaf_rn(sc[2 * i + 1], a, -top));
-              sum[2 * (i & 1)] += u, sum[2 * (i & 1) + 1] += v;
-              w[i] = pack_h2(u, v);
+              const float2 e = __ffma2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), aa, off), w2 = make_float2(ex2(e.x), ex2(e.y));
+              sum[i & 1] = __fadd2_rn(sum[i & 1], w2);
+              w[i] = pack_h2(w2.x, w2.y);
             }
             // the weights over scores that have been read: sixteen columns hold 32 of them
             tmem_st16(lanes + s_col(x, buf) + 16 * half, w);
@@ -260,14 +269,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           tc_wait_ld();
           mask(1, s1);
           weigh(1, s1);
-          den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          den += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           tc_wait_st();
-          if (g > 0) product(g - 1);                 // (not the last one's: that would have it in line with this softmax)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(kPFull + 2 * x + buf));
         }
-        product(g);
+        wait(kODone + 2 * x + ((g - 1) & 1), ((g - 1) >> 1) & 1);
         tc_fence_after();
       }
       // ---- the rows, or this CTA's part of them
@@ -409,66 +417,53 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       }
       left -= take, cur.chunk += take;
     }
-  } else if (warp == kWorkers + kMakers) {
+  } else if (warp < kIssuers + 2) {
     // ================================================================ MMAs.  Everything that addresses them is the same in all lanes, and the compiler can see it (what came
-    // from memory by way of a shuffle): it then lies in uniform registers, and an MMA is issued in its own time instead of 60 cycles.
+    // from memory by way of a shuffle): it then lies in uniform registers.  A warp per tile: one warp for both leaves the tensor core idle in each of its waits, which take 100 to 200
+    // cycles also when there is nothing to wait for (1.41 us per chunk of two tiles).
     constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
     const uint32_t ubase = __shfl_sync(0xffffffffu, base, 0), ubars = ubase + C::kOffBars;
-    const uint64_t q_desc = make_b_desc(ubase), k_desc = make_b_desc(ubase + C::kOffK), v_desc = make_b_desc(ubase + C::kOffV);
-    constexpr uint32_t kQ16 = C::kQBytes / 16, kQHalf16 = 8 * kTile, kK16 = C::kKBytes / 16, kKHalf16 = 8 * kTokens, kV16 = C::kVBytes / 16;
+    const uint64_t q_desc = make_b_desc(ubase + (warp - kIssuers) * C::kQBytes), k_desc = make_b_desc(ubase + C::kOffK), v_desc = make_b_desc(ubase + C::kOffV);
+    constexpr uint32_t kQHalf16 = 8 * kTile, kK16 = C::kKBytes / 16, kKHalf16 = 8 * kTokens, kV16 = C::kVBytes / 16;
     auto ubar = [&](int i) { return ubars + 8 * i; };
+    const int x = warp - kIssuers;
     int k_at = 0, v_at = 0;                          // slots of the next keys and values ...
     uint32_t k_turn = 0, v_turn = 0;                 // ... and the parity of their barriers
-    uint32_t score0 = 0, score1 = 0, weigh0 = 0, weigh1 = 0, segs0 = 0, segs1 = 0;   // chunks of each tile whose scores, whose products have been issued; tiles of queries
-    // scores of the next chunk
-    auto scores = [&](bool two) {
+    uint32_t scored = 0, weighed = 0, tiles = 0;     // chunks whose scores, whose products have been issued; tiles of queries
+    // scores of the next chunk.  (A second tile without rows lets go of the keys and values all the same, when they are there: their barriers count two arrivals.)
+    auto scores = [&](bool active) {
       spin(kKFull + k_at, k_turn);
-      tc_fence_after();
-      const uint64_t k = k_desc + (uint64_t)(k_at * kK16);
-      if (!lost) {
-#pragma unroll
-        for (int h = 0; h < C::kHalves; ++h)
-          mma4_ss(tmem + s_col(0, score0 & 1), q_desc + h * kQHalf16, k + h * kKHalf16, idesc_s, h);
-      }
-      tc_commit(ubar(kSFull + (score0 & 1)));
-      ++score0;
-      if (two) {
+      if (active) {
+        tc_fence_after();
         if (!lost) {
 #pragma unroll
           for (int h = 0; h < C::kHalves; ++h)
-            mma4_ss(tmem + s_col(1, score1 & 1), q_desc + kQ16 + h * kQHalf16, k + h * kKHalf16, idesc_s, h);
+            mma4_ss(tmem + s_col(x, scored & 1), q_desc + h * kQHalf16, k_desc + (uint64_t)(k_at * kK16 + h * kKHalf16), idesc_s, h);
         }
-        tc_commit(ubar(kSFull + 2 + (score1 & 1)));
-        ++score1;
+        tc_commit(ubar(kSFull + 2 * x + (scored & 1)));
+        ++scored;
       }
       tc_commit(ubar(kKFree + k_at));
       if (++k_at == C::kKv) k_at = 0, k_turn ^= 1;
     };
-    for (int left = n; left > 0;) {
+    for (int left = __shfl_sync(0xffffffffu, n, 0); left > 0;) {
       settle<kRows, kTokens>(p, cur);
       const Segment sg = segment(p, cur, left);
-      const int take = min(left, cur.s.chunks - cur.chunk);
+      const int take = __shfl_sync(0xffffffffu, min(left, cur.s.chunks - cur.chunk), 0);
       const int count = __shfl_sync(0xffffffffu, sg.count, 0);
-      const bool two = __shfl_sync(0xffffffffu, sg.rows > kTile, 0);
+      const bool active = __shfl_sync(0xffffffffu, sg.rows > kTile * x, 0);
       if (count > 0) {
-        spin(kQFull, segs0++ & 1);
-        if (two) spin(kQFull + 1, segs1++ & 1);
-        scores(two);
+        if (active) spin(kQFull + x, tiles++ & 1);
+        scores(active);
         for (int j = 0; j < count; ++j) {
-          if (j + 1 < count) scores(two);
+          if (j + 1 < count) scores(active);
           spin(kVFull + v_at, v_turn);
-          const uint64_t v = v_desc + (uint64_t)(v_at * kV16);
-          spin(kPFull + (weigh0 & 1), (weigh0 >> 1) & 1);
-          tc_fence_after();
-          if (!lost) mma4_ts(tmem + o_col(0), tmem + s_col(0, weigh0 & 1), v, idesc_o, j > 0);
-          tc_commit(ubar(kODone + (weigh0 & 1)));
-          ++weigh0;
-          if (two) {
-            spin(kPFull + 2 + (weigh1 & 1), (weigh1 >> 1) & 1);
+          if (active) {
+            spin(kPFull + 2 * x + (weighed & 1), (weighed >> 1) & 1);
             tc_fence_after();
-            if (!lost) mma4_ts(tmem + o_col(1), tmem + s_col(1, weigh1 & 1), v, idesc_o, j > 0);
-            tc_commit(ubar(kODone + 2 + (weigh1 & 1)));
-            ++weigh1;
+            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, weighed & 1), v_desc + (uint64_t)(v_at * kV16), idesc_o, j > 0);
+            tc_commit(ubar(kODone + 2 * x + (weighed & 1)));
+            ++weighed;
           }
           tc_commit(ubar(kVFree + v_at));
           if (++v_at == C::kKv) v_at = 0, v_turn ^= 1;
@@ -477,8 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       left -= take, cur.chunk += take;
     }
     // everything issued is over before the tensor memory is given back, whatever was waited for
-    tc_commit(bar(kDone));
-    for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kDone), 0); ++i) {}
+    tc_commit(bar(kDone + x));
+    for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kDone + x), 0); ++i) {}
   } else {
     // ================================================================ copies: lane i brings block i of the chunk; its page is looked up a chunk ahead
     uint32_t g = 0;
@@ -515,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) {}
   }
   __syncthreads();
-  if (warp == kWorkers + kMakers) tmem_dealloc<512>(tmem);
+  if (warp == kIssuers) tmem_dealloc<512>(tmem);
 }
 
 // The parts of tiles that several CTAs hold, in the order of the list: kJoinRows rows of the tile that begins in share blockIdx.x and does not end there.  (One CTA that arrives last
@@ -551,9 +546,8 @@ int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   const int st = grow_workspace(ctx, reinterpret_cast<void **>(&ctx->at_partials), &ctx->at_partial_bytes, (size_t)(ctas * C::kWorkBytes));
   if (st != ROSAQ_OK) return st;
   p.partials = ctx->at_partials;
-  // Not chained to the launch before it: a CTA takes all of an SM's tensor memory, which a CTA of that launch may still be going to ask for.
-  kern<<<ctas, kThreads, C::kSmem, s>>>(p);
-  if (cudaGetLastError() != cudaSuccess) return ROSAQ_ERR_CUDA;
+  const int launched = kv_launch(kern, dim3(ctas), kThreads, C::kSmem, s, p);
+  if (launched != ROSAQ_OK) return launched;
   return kv_launch(attend_rows_join_kernel<kHd>, dim3(ctas, kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
 }
 
