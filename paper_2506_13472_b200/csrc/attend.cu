@@ -12,13 +12,13 @@
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
 //
-// Bound: memory for one row per sequence.  What moves is the cache, once; a block of 16 tokens and one key/value head (2176 bytes at 4 bits, head of
-// 128) takes a warp about 190 instructions, half of what an SM issues in the time in which its share of the HBM bandwidth delivers the block.
-// The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the
-// device, so a captured launch follows them.  Every warp streams a run
-// of its own through slots of its own and refills them itself.
-// A tile whose blocks several CTAs share is finished by the CTA that arrives last, in the order of the shares: no CTA waits for another, and the
-// bits are the same every time.
+// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, 455 per pair
+// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 132 us, 119 without the
+// arithmetic, 95 at the copy bandwidth.  Short calls are bound by latency: 5.7 us for one chunk, 0.9 to 1.0 us per further chunk of a warp, 5 us to join CTAs.
+// The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the device, so a captured launch
+// follows them.  A CTA's share is cut into one run per warp, each with slots of its own, all filled by one more warp, a lane per slot (warps that fill their own: 153 to 168 us
+// instead of 152).  A tile whose chunks several CTAs share is finished by the CTA that arrives last, in the order of the shares: no CTA waits for another, and the bits are the
+// same every time.
 #include <algorithm>
 
 #include "attend_common.cuh"
@@ -28,10 +28,11 @@ namespace {
 
 constexpr int kChunk = 2, kTokens = kChunk * kKvBlock;   // blocks that a warp takes at a time
 constexpr int kRows = 8;                            // query rows of a tile
-#ifndef MANY
-#define MANY 64
-#endif
-constexpr long long kManyRows = MANY;          // per sequence and key/value head: from here on attend_rows.cu
+// From kManyRows query rows per sequence and key/value head on, and from kManyWork of (row, key/value head, token that the table has room for) in all: attend_rows.cu, which takes 9 us
+// more for any call and a third to a half of the time per row and token.  (us here and there, 32 query and 8 key/value heads of 128 at 4 bits: 32 rows of each of 16 sequences of 1000
+// tokens 35 and 38, 64 rows 48 and 39; of one sequence of 500 tokens 64 rows 12.5 and 22; of 4000 tokens 64 rows 26 and 31, 128 rows 33 and 31; of 30000 tokens 64 rows 65 and 52;
+// 128 rows behind a prefix of 500 tokens 21 and 31, of 4000 41 and 39, of 16000 76 and 49.)
+constexpr long long kManyRows = 64, kManyWork = 1ll << 22;
 
 __device__ __forceinline__ float lg2(float x) {
   float y;
@@ -520,7 +521,8 @@ int launch_few(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
 }
 
 int launch_any(rosaq_ctx *ctx, int hd, int bits, const AtParams &p, long long rows_of_seq, cudaStream_t s) {
-  if (rows_of_seq >= kManyRows) return launch_attend_rows(ctx, p, hd, bits, s);
+  const long long room = p.prefix_tokens > 0 ? p.prefix_tokens : (long long)p.b.ld_table * (kKvBlock << p.kv.page_shift);
+  if (rows_of_seq >= kManyRows && (double)rows_of_seq * p.b.n_seqs * p.kv.n_heads * (double)room >= (double)kManyWork) return launch_attend_rows(ctx, p, hd, bits, s);
   if (hd == 128) return bits == 4 ? launch_few<128, 4>(ctx, p, s) : launch_few<128, 8>(ctx, p, s);
   return bits == 4 ? launch_few<64, 4>(ctx, p, s) : launch_few<64, 8>(ctx, p, s);
 }

@@ -208,8 +208,9 @@ def fill(ctx, rng, held, table, lens, loud=1.0, v_size=1.0, offset=0.0):
 def expect(held, table, lens, new, q, scale, prefix=None):
     """(out, bound) of all rows."""
     group = q.shape[1] // held.width
-    many = lambda rows: rows * group >= 64  # noqa: E731   (from here on the kernel that rounds keys and values to fp16)
-    rounded = many(-(-q.shape[0] // len(lens))) or (prefix is not None and many(q.shape[0]))
+    # the kernel that rounds keys and values to fp16
+    many = lambda rows, seqs, room: rows * group >= 64 and rows * group * seqs * held.n_kv_heads * room >= 1 << 22  # noqa: E731
+    rounded = many(-(-q.shape[0] // len(lens)), len(lens), table.shape[1] * held.page_tokens) or (prefix is not None and many(q.shape[0], 1, prefix[1]))
     outs, bounds, at = [], [], 0
     hd, hq = held.head_dim, q.shape[1] // held.head_dim
     args = (held.pages, held.n_kv_heads, hd, held.bits, held.page_tokens)
@@ -245,10 +246,28 @@ CASES = [
 ]
 
 
-@pytest.mark.parametrize("heads,group,hd,bits,page,lens,new", CASES)
-def test_attend(ctx, heads, group, hd, bits, page, lens, new):
+MANY = [
+    # many query rows per sequence and key/value head, in a table with room for long sequences (which is what the choice of the kernel goes by)
+    (2, 1, 64, 8, 16, [150], [150]),                                    # a prompt
+    (2, 2, 128, 4, 256, [5000, 1, 900], [130, 1, 64]),
+    (1, 64, 128, 4, 64, [1], [1]),                                      # one token that all rows see
+    (3, 16, 128, 8, 16, [15, 16, 17, 64, 65, 0, 700], [4, 4, 4, 4, 17, 0, 4]),   # ends of blocks and pages
+    (1, 7, 64, 4, 32, [63, 64, 65, 129, 200], [40, 64, 20, 8, 30]),     # chunks, odd groups, tiles that end anywhere
+    (5, 2, 64, 4, 128, [300] * 40, [37] * 40),                          # more tiles than CTAs
+    (1, 2, 128, 4, 1024, [70000], [100]),                               # one tile over all CTAs
+    (2, 3, 128, 8, 64, [600, 600], [600, 100]),                         # rows that see next to nothing beside rows that see all
+]
+
+
+@pytest.mark.parametrize("heads,group,hd,bits,page,lens,new,wide", [(*c, False) for c in CASES] + [(*c, True) for c in MANY])
+def test_attend(ctx, heads, group, hd, bits, page, lens, new, wide):
     rng = np.random.default_rng(heads + 10 * group + sum(lens))
     held, table = filled(rng, heads, hd, bits, page, lens)
+    if wide:
+        rows = -(-sum(new) // len(lens)) * group
+        assert rows >= 64
+        room = -(-(1 << 22) // (rows * len(lens) * heads * page))
+        table = np.pad(table, ((0, 0), (0, max(0, room - table.shape[1]))), constant_values=-5)
     fill(ctx, rng, held, table, lens, loud=5.0)
     rows, d = sum(new), heads * group * hd
     wide = d + 16
@@ -278,6 +297,9 @@ def test_attend(ctx, heads, group, hd, bits, page, lens, new):
     (8, 4, 128, 4, 64, 2500, [i % 40 + 1 for i in range(64)], [1] * 64),
     (2, 8, 64, 8, 16, 333, [30, 9, 400], [3, 9, 20]),
     (1, 3, 128, 8, 32, 4096, [40], [40]),
+    (1, 3, 128, 8, 32, 40000, [40], [40]),                              # many rows behind the prefix from here on
+    (2, 8, 64, 4, 16, 9001, [3, 1, 0, 70, 9], [3, 1, 0, 30, 9]),
+    (8, 4, 128, 4, 64, 4100, [i % 40 + 1 for i in range(33)], [1] * 33),
 ])
 def test_attend_prefix(ctx, heads, group, hd, bits, page, prefix, lens, new):
     rng = np.random.default_rng(prefix + sum(lens))
