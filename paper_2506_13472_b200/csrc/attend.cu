@@ -107,11 +107,12 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
   }
   if (threadIdx.x < 2 * kWarps + 2) parts[threadIdx.x].from = kNoTile;
   grid_dep_launch_dependents();
-  __syncthreads();
   grid_dep_wait();                                  // q, the batch, the pages, the partial tiles: all may be the previous kernel's
 
-  Share share;
-  if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, 8 * kWarps, kWarps, blockIdx.x == 0 && warp == 0, share)) return;
+  __shared__ Share share;                           // (by one warp: eight that compute the same take turns)
+  if (warp == 0) find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, 8 * kWarps, kWarps, blockIdx.x == 0, share);
+  __syncthreads();
+  if (share.begin == share.end) return;
   Cursor cur = share.cur;
   const int n = (int)(share.end - share.begin);     // chunks of this CTA (a share of 2^31 would be 4 TB of cache)
   // warp w takes chunks [n w / kWarps, n (w + 1) / kWarps) of them, rounded up (warp 0 always has one): long runs, so that a warp seldom changes its tile and never waits for another

@@ -110,15 +110,16 @@ struct Shares {
   __device__ __forceinline__ int last(long long at, int chunks) const { return max(first(at, chunks), owner(at + max(chunks - 1 - near, 0))); }
 };
 
-// What CTA `cta` of at most `most` does: chunks [begin, end) of the list, `cur` at the first one.  A whole warp.  A CTA takes at least `least` chunks, and tiles of fewer than
-// `few` on average are not cut.  False: nothing.
+// What CTA `cta` of at most `most` does: chunks [begin, end) of the list (none if they are equal), `cur` at the first one.  A whole warp, `out` in shared memory.  A CTA takes at
+// least `least` chunks, and tiles of fewer than `few` on average are not cut.
 struct Share {
   Shares all;
   long long begin, end;
   Cursor cur;
 };
 template <int kRows, int kTokens>
-__device__ __forceinline__ bool find_share(const AtParams &p, int cta, int most, int few, int least, bool report, Share &out) {
+__device__ __forceinline__ void find_share(const AtParams &p, int cta, int most, int few, int least, bool report, Share &out) {
+  if ((threadIdx.x & 31) == 0) out.begin = out.end = 0;
   const int lane = threadIdx.x & 31;
   long long total = 0;
   int units = 0, longest = 0;
@@ -134,11 +135,11 @@ __device__ __forceinline__ bool find_share(const AtParams &p, int cta, int most,
     longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, d));
   }
   units *= p.kv.n_heads;
-  if (total == 0) return false;
-  Shares &sh = out.all;
+  if (total == 0) return;
+  Shares sh;
   sh.total = total;
   sh.ctas = (int)min((long long)most, total < (long long)few * units ? (long long)units : max(divide(total, least), 1ll));
-  if (cta >= sh.ctas) return false;
+  if (cta >= sh.ctas) return;
   sh.part = divide(total, sh.ctas), sh.left = (int)(total - sh.part * sh.ctas);
   sh.near = (longest + 1) / 2;
   if (sh.near > min(8ll, sh.part / 8)) sh.near = 0;
@@ -167,19 +168,19 @@ __device__ __forceinline__ bool find_share(const AtParams &p, int cta, int most,
   cur.s = load_seq<kRows, kTokens>(p, cur.seq, false);
   cur.unit = (int)divide(even - base, cur.s.chunks), cur.chunk = (int)((even - base) - (long long)cur.unit * cur.s.chunks);
   const int moved = sh.snap(cur.chunk, cur.s.chunks);
-  out.begin = even + moved, cur.chunk += moved;
+  const long long begin = even + moved;
+  cur.chunk += moved;
   // and where the next CTA's begins, by the same rule
-  out.end = total;
+  long long end = total;
   if (cta + 1 < sh.ctas) {
     const long long next = sh.even(cta + 1);
     Cursor c = cur;
-    c.chunk += (int)(next - out.begin);
+    c.chunk += (int)(next - begin);
     settle<kRows, kTokens>(p, c);
-    out.end = next + sh.snap(c.chunk, c.s.chunks);
+    end = next + sh.snap(c.chunk, c.s.chunks);
   }
   settle<kRows, kTokens>(p, cur);
-  out.cur = cur;
-  return true;
+  if (lane == 0) out.all = sh, out.begin = begin, out.end = end, out.cur = cur;
 }
 
 // A finished row: its place in out and in what the prefix launch found.

@@ -120,18 +120,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   // The launch before this one is over before the tensor memory is asked for, and those behind begin when this CTA has it: a CTA takes all that an SM has, and neither side may
   // hold what the other one waits for.
   grid_dep_wait();
-  Share share;
+  __shared__ Share share;
   OpenRows *const open = reinterpret_cast<OpenRows *>(p.partials + 2ll * gridDim.x * at_partial(kHd, kRows)) + blockIdx.x;
-  if (threadIdx.x == 0) open->rows = 0;
-  if (!find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, kFew, kLeast, blockIdx.x == 0 && warp == 0, share)) return;
-  Cursor cur = share.cur;
-  const int n = (int)(share.end - share.begin);
   if (warp == kIssuers) tmem_alloc<512>(smem_u32(tmem_at));
+  if (warp == 0) {
+    if (lane == 0) open->rows = 0;
+    find_share<kRows, kTokens>(p, blockIdx.x, gridDim.x, kFew, kLeast, blockIdx.x == 0, share);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_at, 0);
   grid_dep_launch_dependents();
+  if (share.begin == share.end) {
+    if (warp == kIssuers) tmem_dealloc<512>(tmem);
+    return;
+  }
+  Cursor cur = share.cur;
+  const int n = (int)(share.end - share.begin);
 
   // A wait that expires is reported, and the warp waits no more: it goes on through what the others rely on.
   bool lost = false;
@@ -160,7 +166,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     const int x = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     const float a = fmaxf(fabsf(p.scale_log2), 1e-30f);   // (its sign is in the queries)
-    const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : p.scale_log2 == 0.f ? 0.f : 1.f);
     uint32_t g = 0;                                  // chunks of this tile so far
     // Products of chunk k end phase k / 2 of one of two barriers.  A phase is waited for only when the one before it on its barrier is known to have ended: chunk g waits for those
     // of chunk g - 2, and those of chunk g - 1 only when it rescales.
@@ -175,26 +180,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       if (active && sg.count > 0) {
         // ---- the queries
         const __half *const src = p.q + (long long)(s.row + tok) * p.ldq + (long long)(sg.head * p.group + (valid ? flat - tok * p.group : 0)) * kHd;
-        // (kLanes lanes per row, so that a row's bytes are read together)
+        // (kLanes lanes per row, so that a row's bytes are read together; a loop of few instructions, which are fetched for the first time here)
         constexpr int kLanes = kHd / 8, kPer = 32 / kLanes;
         const int piece = lane % kLanes;
-#pragma unroll
-        for (int i0 = 0; i0 < 32 / kPer; i0 += 8) {
-          uint4 v[8];                                // (all loads before the first store, which might be to their memory for all the compiler knows)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int of = kPer * (i0 + i) + lane / kLanes;
-            const __half *const from = reinterpret_cast<const __half *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), of));
-            const bool there = __shfl_sync(0xffffffffu, valid, of);
-            v[i] = there ? *reinterpret_cast<const uint4 *>(from + 8 * piece) : make_uint4(0, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int to = 32 * (warp & 3) + kPer * (i0 + i) + lane / kLanes;
-            __half2 *const h = reinterpret_cast<__half2 *>(&v[i]);
+        uint8_t *const rows = smem + x * C::kQBytes + (piece / 8) * (128 * kTile);
+#pragma unroll 1
+        for (int i = 0; i < 32; i += kPer) {
+          const int of = i + lane / kLanes, to = 32 * (warp & 3) + of;
+          const __half *const from = reinterpret_cast<const __half *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), of));
+          const int bytes = __shfl_sync(0xffffffffu, valid, of) ? 16 : 0;   // (the others are zeros)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(rows + 128 * to + (((piece & 7) ^ (to & 7)) << 4))), "l"(from + 8 * piece), "r"(bytes)
+                       : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (p.scale_log2 <= 0.f) {
+          const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : 0.f);
+#pragma unroll 1
+          for (int i = 0; i < 32; i += kPer) {
+            const int to = 32 * (warp & 3) + i + lane / kLanes;
+            __half2 *const h = reinterpret_cast<__half2 *>(rows + 128 * to + (((piece & 7) ^ (to & 7)) << 4));
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = __hmul2(h[e], sign);
-            *reinterpret_cast<uint4 *>(smem + x * C::kQBytes + (piece / 8) * (128 * kTile) + 128 * to + (((piece & 7) ^ (to & 7)) << 4)) = v[i];
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -317,7 +323,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           for (int e = 0; e < 32; e += 4)
             *reinterpret_cast<float4 *>(stage + 128 * lane + (((e / 4) ^ (lane & 7)) << 4)) = make_float4(o[e] * f, o[e + 1] * f, o[e + 2] * f, o[e + 3] * f);
           __syncwarp();
+          if (!sg.whole) {
+            float *const part = sums + (lane / 8 - lane) * kHd + ch + 4 * (lane & 7);
 #pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int of = 4 * i + lane / 8;
+              if (r - lane + of < sg.rows) *reinterpret_cast<float4 *>(part + 4 * i * kHd) = *reinterpret_cast<const float4 *>(stage + 128 * of + (((lane & 7) ^ (of & 7)) << 4));
+            }
+            continue;
+          }
+#pragma unroll 2
           for (int i = 0; i < 8; ++i) {
             const int of = 4 * i + lane / 8, at = ch + 4 * (lane & 7);
             float4 v = *reinterpret_cast<const float4 *>(stage + 128 * of + (((lane & 7) ^ (of & 7)) << 4));
@@ -534,7 +549,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_rows_join_kernel(const __
 template <int kHd, int kBits>
 int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   using C = RCfg<kHd, kBits>;
-  static_assert(C::kSmem <= 227 * 1024 && 8 * kBars + 16 <= 512, "shared memory");
+  static_assert(C::kSmem + (int)sizeof(Share) <= 227 * 1024 && 8 * kBars + 16 <= 512, "shared memory");
   auto *const kern = attend_rows_kernel<kHd, kBits>;
   int &ready = ctx->at_per_sm[4 + (kHd == 64) + 2 * (kBits == 8)];
   if (ready == 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
