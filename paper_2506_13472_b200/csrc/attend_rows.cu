@@ -428,7 +428,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar((value ? kVFull : kKFull) + st)), mbar_arrive(bar(kRawEmpty + raw));
+        if (lane == 0) mbar_arrive(bar((value ? kVFull : kKFull) + st));
+        if (lane == 0 && !lost) mbar_arrive(bar(kRawEmpty + raw));   // (a slot whose copy was given up on is not filled again)
       }
       left -= take, cur.chunk += take;
     }
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     }
     // everything issued is over before the tensor memory is given back, whatever was waited for
     tc_commit(bar(kDone + x));
-    for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kDone + x), 0); ++i) {}
+    for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kDone + x), 0); ++i) __nanosleep(100);
   } else {
     // ================================================================ copies: lane i brings block i of the chunk; its page is looked up a chunk ahead
     uint32_t g = 0;
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
     }
     // the CTA outlasts its copies, also when nobody waits for them any more
     for (uint32_t k = g < (uint32_t)C::kRaw ? 0 : g - C::kRaw; k < g; ++k)
-      for (int i = 0; i < 1 << 20 && !mbar_try_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) {}
+      for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) __nanosleep(100);
   }
   __syncthreads();
   if (warp == kIssuers) tmem_dealloc<512>(tmem);

@@ -514,14 +514,15 @@ def test_two_contexts_at_once(ctx):
     other.close()
 
 
-def test_attend_gives_up_in_time(ctx):
+@pytest.mark.parametrize("new,bits", [(1, 4), (20, 4), (20, 8)])
+def test_attend_gives_up_in_time(ctx, new, bits):
     """A wait limit of one poll: whatever the launch makes of it, it ends, says so or is right, and the next call is as ever."""
     rng = np.random.default_rng(13)
-    lens = [9000, 40]
-    held, table = filled(rng, 2, 128, 4, 64, lens)
+    lens = [20000, 40]
+    held, table = filled(rng, 2, 128, bits, 64, lens)
     fill(ctx, rng, held, table, lens)
-    q = torch.randn((2, 8 * 128), device="cuda").half()
-    batch = rb.KvBatch(ints([0, 1, 2]), ints(lens), ints(table.tolist()))
+    q = torch.randn((2 * new, 8 * 128), device="cuda").half()
+    batch = rb.KvBatch(ints([0, new, 2 * new]), ints(lens), ints(table.tolist()))
     want = ctx.attend(q, held, batch).clone()
     limit = ctx.set_wait_limit(1)
     got = ctx.attend(q, held, batch)
@@ -529,3 +530,76 @@ def test_attend_gives_up_in_time(ctx):
     ctx.set_wait_limit(limit)
     assert status == rb.ROSAQ_ERR_TIMEOUT or (status == rb.ROSAQ_OK and same(got, want))
     assert same(ctx.attend(q, held, batch), want) and ctx.last_status() == rb.ROSAQ_OK
+
+
+def test_calls_of_two_graphs_share_a_context(ctx):
+    """A prompt's graph and a decoding step's, captured apart, replayed in turn with calls in between: one context's workspaces, outgrown ones among them."""
+    rng = np.random.default_rng(14)
+    own = rb.Context(0)
+    lens = [5000, 9000]
+    held, table = filled(rng, 4, 128, 4, 64, lens)
+    fill(ctx, rng, held, table, lens)
+    tab, n, pre = ints(table.tolist()), ints(lens), (ints(table[1].tolist()), 8999)
+    calls = [(60, rb.KvBatch(ints([0, 60, 120]), n, tab)), (1, rb.KvBatch(ints([0, 1, 2]), n, tab)),
+             (30, rb.KvBatch(ints([0, 30, 60]), n, tab, prefix=pre))]
+    qs = [torch.randn((2 * m, 16 * 128), device="cuda").half() for m, _ in calls]
+    want = [ctx.attend(q, held, b).clone() for q, (_, b) in zip(qs, calls)]
+    side, graphs, outs = torch.cuda.Stream(), [], []
+    for i in (1, 0, 2):                                       # the smallest workspaces first
+        q, b = qs[i], calls[i][1]
+        side.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            own.attend(q, held, b)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=side):
+            outs.append((i, own.attend(q, held, b)))
+        graphs.append(g)
+    for turn in range(3):
+        for (i, out), g in zip(outs, graphs):
+            out.zero_()
+            g.replay()
+            assert same(own.attend(qs[turn], held, calls[turn][1]), want[turn])
+            assert same(out, want[i]), (turn, i)
+    assert own.last_status() == rb.ROSAQ_OK
+    own.close()
+
+
+@pytest.mark.parametrize("new", [2, 40])
+@pytest.mark.parametrize("scale", [-0.11, 0.0, 1e-30])
+def test_attend_scales(ctx, new, scale):
+    """Scales below zero, at it and next to it, on both kernels."""
+    rng = np.random.default_rng(15)
+    lens = [33000]
+    held, table = filled(rng, 2, 64, 8, 64, lens)
+    fill(ctx, rng, held, table, lens)
+    q = torch.randn((new, 4 * 64), device="cuda").half()
+    batch = rb.KvBatch(ints([0, new]), ints(lens), ints(table.tolist()))
+    out = ctx.attend(q, held, batch, scale=scale)
+    want, bound = expect(held, table, lens, [new], q, scale)
+    inside(out, want, bound)
+
+
+def test_many_rows_that_are_no_numbers(ctx):
+    """As above, where a row shares its tile with others; and pairs behind the last token."""
+    rng = np.random.default_rng(16)
+    lens, new = [8200, 90], [70, 70]
+    held, table = filled(rng, 4, 128, 4, 64, lens)
+    fill(ctx, rng, held, table, lens)
+    raw = held.pages.view(held.pages.shape[0], 4, 4, -1)
+    for i, n in enumerate(lens):
+        block = raw[table[i, n // 64], :, n % 64 // 16]
+        pairs = block[:, 2048:].clone().view(torch.int16).view(4, 2, 16, 2)
+        pairs[:, :, n % 16:] = ints([0x7c00, 0x7e00]).to(torch.int16)
+        block[:, 2048:] = pairs.view(4, 64).view(torch.uint8).view(4, 128)
+    q = torch.from_numpy(rng.standard_normal((140, 4 * 128)).astype(np.float16)).cuda()
+    batch = rb.KvBatch(ints([0, 70, 140]), ints(lens), ints(table.tolist()))
+    clean = ctx.attend(q, held, batch)
+    want, bound = expect(held, table, lens, new, q, 128 ** -0.5)
+    inside(clean, want, bound)
+    q[1, 5], q[69, 128], q[139, 300] = float("nan"), float("inf"), float("-inf")
+    got = ctx.attend(q, held, batch).view(140, 4, 128)
+    bad = torch.zeros((140, 4), dtype=torch.bool, device="cuda")
+    bad[1, 0] = bad[69, 1] = bad[139, 2] = True
+    assert torch.equal(torch.isnan(got).any(-1), bad) and torch.equal(torch.isnan(got).all(-1), bad)
+    inside(got[~bad], want.view(140, 4, 128)[~bad], bound.view(140, 4, 128)[~bad])
