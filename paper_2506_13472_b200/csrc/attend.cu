@@ -5,9 +5,9 @@
 // So no key is dequantised: nibbles and bytes, masked out of their words, ARE fp16 numbers (subnormal: code * 2^-24), exact operands of the
 // tensor core.  Value codes are taken about the middle of their range, d_t - 2^(bits - 1), which costs an addition per pair and keeps the sums as small as
 // the result: of positive codes the roundings of the weights and of the accumulators would all point one way (against 64 bits, 26000 tokens
-// at 8 bits: 1.2e-3 that way).  The weights of the second product are kept near one whatever the size of the values: with 2^e the power of two in s_t,
-// u_t = score_t log2(e) + e is what the running maximum M is taken of, and p_t s_t = 2^(u_t - M) (s_t 2^-e) has its greatest value in [1, 2)
-// before the rounding to fp16 (2^-11 relative, 2^-25 of the greatest weight absolute), while sum(p_t) and sum(p_t lo_t) stay in fp32.
+// at 8 bits: 1.2e-3 that way).  The weights of the second product keep their size whatever that of the values: u_t = score_t log2(e) + log2(s_t) is what the
+// running maximum is taken of, so that p_t s_t has its greatest value between 2^10 and 2^15 before the rounding to fp16 (2^-11 relative, 2^-35 of the
+// greatest weight absolute), while sum(p_t) and sum(p_t lo_t) stay in fp32.
 //
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
@@ -34,11 +34,6 @@ constexpr int kRows = 8;                            // query rows of a tile
 // 128 rows behind a prefix of 500 tokens 21 and 31, of 4000 41 and 39, of 16000 76 and 49.)
 constexpr long long kManyRows = 64, kManyWork = 1ll << 22;
 
-__device__ __forceinline__ float lg2(float x) {
-  float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -49,16 +44,15 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// A fragment of step j of a block in units of 2^-24.  Four bits, keys (token, channel): the codes, of channels 8-15 sixteen times the codes.  Four bits, values (channel,
-// token): the whole bytes, i.e. code + 16 * (code of the channel eight further on), in the rows of channels 0-7, sixteen times the code in those of channels 8-15; what
-// is too much in the first is taken off the sums (one operation less per word).
+// A fragment of step j of a block, keys (token, channel) or values (channel, token), in units of 2^-24: the codes; at four bits sixteen times the codes of the second nibbles, which
+// are channels 8-15.  (Values: whole bytes in the rows of channels 0-7, what is too much taken off at the end, are an operation less per word; but what the accumulators cut off
+// is relative to the sixteenfold sum then: 131071 tokens 3.2e-4 off instead of 2.x.)
 template <int kBits, bool kValue>
 __device__ __forceinline__ void code_fragment(const uint32_t *w, int j, uint32_t *a) {
-  if (kBits == 4 && kValue) {
-    a[0] = w[j] & 0x00ff00ffu, a[1] = w[j] & 0x00f000f0u, a[2] = __byte_perm(w[j], 0, 0x4341), a[3] = a[2] & 0x00f000f0u;
-  } else if (kBits == 4) {
+  if (kBits == 4) {
     const uint32_t u = w[j], v = u >> 8;
-    a[0] = u & 0x000f000fu, a[2] = u & 0x00f000f0u, a[1] = v & 0x000f000fu, a[3] = v & 0x00f000f0u;
+    const uint32_t a1 = u & 0x00f000f0u, a2 = v & 0x000f000fu;
+    a[0] = u & 0x000f000fu, a[1] = kValue ? a1 : a2, a[2] = kValue ? a2 : a1, a[3] = v & 0x00f000f0u;
   } else {
     const uint32_t u = w[2 * j], v = w[2 * j + 1];
     a[0] = __byte_perm(u, 0, 0x4140), a[1] = __byte_perm(v, 0, 0x4140), a[2] = __byte_perm(u, 0, 0x4342), a[3] = __byte_perm(v, 0, 0x4342);
@@ -346,7 +340,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
           for (int e = 0; e < 2; ++e) {
             float m = most[e];
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4)), m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-            m = fmaxf(fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)), top[e]);
+            m = fmaxf(fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) - kUp, top[e]);
             const float f = ex2(top[e] - m);
             top[e] = m, den[e] *= f, off[e] *= f;
 #pragma unroll
@@ -358,16 +352,17 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
 #pragma unroll
         for (int b = 0; b < kChunk; ++b) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = ex2(sc[b][e] - top[e & 1]);
-            den[e & 1] = __fmaf_rn(x, vi[b][e >> 1], den[e & 1]);
-            off[e & 1] = __fmaf_rn(x, vl[b][e >> 1], off[e & 1]);
-            sc[b][e] = x;
+          for (int h = 0; h < 2; ++h) {
+            // (the sums are those of the rounded weights: where few tokens have all the weight, their roundings cancel)
+            const uint32_t w = pack_h2(ex2(sc[b][2 * h] - top[0]), ex2(sc[b][2 * h + 1] - top[1]));
+            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+            den[0] = __fmaf_rn(x.x, vi[b][h], den[0]), den[1] = __fmaf_rn(x.y, vi[b][h], den[1]);
+            off[0] = __fmaf_rn(x.x, vl[b][h], off[0]), off[1] = __fmaf_rn(x.y, vl[b][h], off[1]);
+            pf[b][h] = transpose8(w);
           }
-          pf[b][0] = transpose8(pack_h2(sc[b][0], sc[b][1])), pf[b][1] = transpose8(pack_h2(sc[b][2], sc[b][3]));
         }
-        // minus the middle of what the fragments hold: 8 + 16 * 8 and 16 * 8, or 128
-        const uint32_t mid[4] = {kBits == 4 ? 0x80888088u : 0x80808080u, 0x80808080u, kBits == 4 ? 0x80888088u : 0x80808080u, 0x80808080u};
+        // minus the middle of what the fragments hold: 8 and 16 * 8, or 128
+        const uint32_t mid[4] = {kBits == 4 ? 0x80088008u : 0x80808080u, 0x80808080u, kBits == 4 ? 0x80088008u : 0x80808080u, 0x80808080u};
 #pragma unroll
         for (int b = 0; b < kChunk; ++b) mma16816(low, mid, pf[b][0], pf[b][1]);
 #pragma unroll
@@ -404,7 +399,6 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
       for (int d = 4; d < 32; d *= 2) den[e] += __shfl_xor_sync(0xffffffffu, den[e], d), off[e] += __shfl_xor_sync(0xffffffffu, off[e], d);
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
-        if (kBits == 4) acc[k][e] -= acc[k][e + 2];
         acc[k][e] *= 16777216.f, acc[k][e + 2] *= kBits == 4 ? 1048576.f : 16777216.f;
       }
       if (!whole) {

@@ -8,8 +8,11 @@
 
 namespace rosaq {
 
-constexpr float kNone = -1e30f;                     // running maximum of a row that has seen nothing
-constexpr float kGrow = 8.f;                        // a maximum is renewed when it is exceeded by this factor of two
+// Weights are exponentials of u - top (base 2), top a value kUp below the greatest u when it was last renewed: the greatest weight is 2^kUp then, and top is renewed when one would
+// pass 2^kGrow, which fp16 still holds.  A long context has most of its weight in tokens far below the greatest, and fp16 is subnormal from 2^-14 on (against 64 bits, 131071 tokens
+// at 4 bits: 3.5e-4 with a greatest weight of one).
+constexpr float kNone = -1e30f;                     // top of a row that has seen nothing
+constexpr float kUp = 10.f, kGrow = 15.f;
 
 struct AtParams {
   KvView kv;
@@ -54,6 +57,11 @@ __device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ uint32_t pack_h2(float a, float b) {

@@ -1,14 +1,20 @@
 // rosaq_attend for many query rows per sequence and key/value head: a prompt, or a batch behind a shared prefix.
 //
-// Bound: the tensor core, so it is tcgen05 here: per chunk of 64 tokens S = Q K^T (128 rows x 64 tokens, both operands in shared memory) and O += P V (P in tensor memory over its
-// scores, V in shared memory), fp32 accumulators in tensor memory.  A CTA has up to two tiles of 128 rows, which share every key and value that eight warps make of the codes:
-// lo + scale * code in one fp16 fused multiply-add, i.e. rounded once to fp16 (2^-11; as are the softmax weights), in the fragment order of the cache's words, so that one stmatrix
-// stores four 8 x 8 pieces: rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  While the tensor core
-// works on one tile's chunk, four warps do the softmax of the other's, a row per thread; the scores of the next chunk go to a second buffer.  The maximum of a row is renewed only
-// when it is exceeded by 2^8: then its accumulators are rescaled in tensor memory.
+// tcgen05: per chunk of 64 tokens S = Q C^T (128 rows x 64 tokens, both operands in shared memory) and O += P D (P in tensor memory over its scores, D in shared memory), fp32
+// accumulators in tensor memory.  C and D are the codes less the middle of their range (8 or 128), exact in fp16, so nothing but the softmax weights is rounded (2^-11), as in
+// attend.cu; with A = scale s_k, B = scale (lo_k + middle s_k), L = log2 s_v, M = lo_v / s_v + middle of a token (scale: with log2 e)
+//   u = A S + (B sum(q) + L),   p s_v = 2^(u - top),   out = (sum (p s_v) D + sum (p s_v) M) / sum (p s_v) / s_v.
+// (Keys and values rounded to fp16 instead need none of the terms: 1.25 us per chunk of 256 rows, and an error of 6.5e-4 where this has 2.8e-4 and the rounding of the result alone
+// 2.1e-4: some channels of keys are several times larger than others, and their roundings move the scores.)
+// A CTA has up to two tiles of 128 rows, which share the operands that four warps make of the codes, in the fragment order of the cache's words: one stmatrix stores four 8 x 8
+// pieces, rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  Softmax: a row per thread, four warps per
+// tile; the scores of the next chunk go to a second buffer.  What the weights of a row are relative to is seldom renewed: then its accumulators are rescaled in tensor memory.
 //
-// Per chunk and pair of tiles: 1056 cycles of MMA, 1024 of exponentials (16 per cycle and SM), about 1000 issue slots of the four schedulers.
+// Measured: 1.65 us per chunk and pair of tiles (head of 128), 3100 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
+// channels 64), the exponentials 1024, the terms 2560 of the shared memory's bandwidth (20 bytes per row and token: a broadcast costs as much as any load).  Before the first chunk
+// and behind the last one about 8 us: the share, the queries and the first codes 4, the rows 4 (135 KB of partial sums per CTA).
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_common.cuh"
 
@@ -18,11 +24,16 @@ namespace {
 constexpr int kTile = 128, kRows = 2 * kTile;       // query rows of an MMA, of a CTA's tile
 constexpr int kTokens = 64, kBlocks = kTokens / kKvBlock;
 constexpr int kWorkers = 8;                         // softmax warps
-constexpr int kMakers = 8;                           // four of keys, four of values
+constexpr int kMakers = 4;                          // a block of sixteen tokens each
 constexpr int kIssuers = kWorkers + kMakers;        // first of the two warps that issue MMAs, one per tile
-constexpr int kThreads = 32 * (kIssuers + 3);
+constexpr int kThreads = 32 * (kIssuers + 4);        // (whole groups of four warps, which registers are shared out to; the last one waits at the end)
+constexpr int kRegsSoftmax = 176, kRegsMaker = 80, kRegsRest = 80;   // 512 in all
+static_assert(2 * kRegsSoftmax + kRegsMaker + kRegsRest <= 512, "registers");
 constexpr int kFew = 16, kLeast = 4;                // chunks: of tiles that are not cut, of a CTA
 constexpr int kJoinRows = 16, kJoinThreads = 256;
+
+// What the pairs of a chunk's tokens come to, two tokens (t, t + 1) at a time: {A_t, A_t+1, B_t, B_t+1}, {1 / s_v twice, M twice}, and behind both L of all
+constexpr int kTermBytes = kTokens * 20;
 
 // A tile that begins in a CTA's share and does not end there, for the launch that joins the parts: behind the partial tiles of all CTAs, one per CTA.
 struct OpenRows {
@@ -37,7 +48,8 @@ struct RCfg {
   static constexpr int kRawBytes = kBlocks * kv_block_bytes(kHd, kBits);
   static constexpr int kRaw = kBits == 4 ? 6 : kHd == 64 ? 4 : 3;   // chunks of codes under way: three of 8.7 KB do not cover the latency of the memory
   static constexpr int kKv = 3;                     // chunks of keys and values: with two, the makers wait for the tensor core and it for them
-  static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + kKv * kKBytes, kOffRaw = kOffV + kKv * kVBytes, kOffBars = kOffRaw + kRaw * kRawBytes;
+  static constexpr int kOffK = 2 * kQBytes, kOffV = kOffK + kKv * kKBytes, kOffRaw = kOffV + kKv * kVBytes, kOffTerms = kOffRaw + kRaw * kRawBytes,
+                       kOffBars = kOffTerms + kKv * kTermBytes;
   static constexpr int kSmem = kOffBars + 512 + 1024;   // (the swizzled operands start at a multiple of 1024)
   static constexpr long long kWorkBytes = 2 * 4 * at_partial(kHd, kRows) + (int)sizeof(OpenRows);   // of a CTA
 };
@@ -162,11 +174,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
   };
 
   if (warp < kWorkers) {
+    reg_inc<kRegsSoftmax>();
     // ================================================================ softmax: warps 0-3 the first tile, 4-7 the second; a row per thread
     const int x = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const float a = fmaxf(fabsf(p.scale_log2), 1e-30f);   // (its sign is in the queries)
-    uint32_t g = 0;                                  // chunks of this tile so far
+    uint32_t g = 0, all = 0;                         // chunks of this tile so far, of both
     // Products of chunk k end phase k / 2 of one of two barriers.  A phase is waited for only when the one before it on its barrier is known to have ended: chunk g waits for those
     // of chunk g - 2, and those of chunk g - 1 only when it rescales.
     for (int left = n; left > 0;) {
@@ -176,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       const int take = min(left, s.chunks - cur.chunk), flat = sg.tile * kRows + kTile * x + row;
       const bool active = sg.rows > kTile * x, valid = kTile * x + row < sg.rows;
       const int tok = valid ? flat / p.group : 0;
-      float top = kNone, den = 0.f;
+      float top = kNone, den = 0.f, off = 0.f;
       if (active && sg.count > 0) {
         // ---- the queries
         const __half *const src = p.q + (long long)(s.row + tok) * p.ldq + (long long)(sg.head * p.group + (valid ? flat - tok * p.group : 0)) * kHd;
@@ -193,56 +205,81 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
                        : "memory");
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (p.scale_log2 <= 0.f) {
-          const __half2 sign = __float2half2_rn(p.scale_log2 < 0.f ? -1.f : 0.f);
-#pragma unroll 1
-          for (int i = 0; i < 32; i += kPer) {
-            const int to = 32 * (warp & 3) + i + lane / kLanes;
-            __half2 *const h = reinterpret_cast<__half2 *>(rows + 128 * to + (((piece & 7) ^ (to & 7)) << 4));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = __hmul2(h[e], sign);
-          }
-        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kQFull + x));
+        float sum_q = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < kLanes; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4 *>(smem + x * C::kQBytes + (i / 8) * (128 * kTile) + 128 * row + (((i & 7) ^ (row & 7)) << 4));
+          const __half2 *const h = reinterpret_cast<const __half2 *>(&v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum_q += __low2float(h[k]) + __high2float(h[k]);
+        }
         const int lim = p.prefix_tokens > 0 ? s.len : valid ? min(max(s.len - s.rows + 1 + tok, 0), s.len) : s.len;
         const int least = __reduce_min_sync(0xffffffffu, lim);
         for (int j = 0; j < sg.count; ++j, ++g) {
           const int buf = g & 1, tok0 = (sg.chunk0 + j) * kTokens;
-          // Scores of this chunk, and products of the last but one before it (which are older): both asked for at once, as an answer takes more than 100 cycles.
+          // Scores of this chunk, terms of its tokens, and products of the last but one before it (which are older): asked for at once, as an answer takes more than 100 cycles.
+          const uint32_t slot = (all + j) % C::kKv, turn = (all + j) / C::kKv;
           {
-            bool here = lost || mbar_try_wait(bar(kSFull + 2 * x + buf), (g >> 1) & 1), old = lost || g < 2 || mbar_try_wait(bar(kODone + 2 * x + buf), ((g >> 1) - 1) & 1);
-            if (!__all_sync(0xffffffffu, here && old)) {
+            // (the scores first: once they are there, the terms three chunks back are, and the parity is that of this chunk)
+            const bool here = lost || mbar_try_wait(bar(kSFull + 2 * x + buf), (g >> 1) & 1), made = lost || mbar_try_wait(bar(kVFull + slot), turn & 1),
+                       old = lost || g < 2 || mbar_try_wait(bar(kODone + 2 * x + buf), ((g >> 1) - 1) & 1);
+            if (!__all_sync(0xffffffffu, here && made && old)) {
               wait(kSFull + 2 * x + buf, (g >> 1) & 1);
+              wait(kVFull + slot, turn & 1);
               if (g >= 2) wait(kODone + 2 * x + buf, ((g >> 1) - 1) & 1);
             }
           }
           tc_fence_after();
-          // The scores are read twice rather than held: registers for the makers' warps.
+          const float4 *const t_ab = reinterpret_cast<const float4 *>(smem + C::kOffTerms + slot * kTermBytes), *const t_vm = t_ab + kTokens / 2, *const t_l = t_vm + kTokens / 2;
+          // u, two tokens at a time; those of the second half go back to tensor memory until the first half's exponentials are done
           const bool border = tok0 + kTokens > least;
-          auto load = [&](int half, float *sc) {
+          const float2 q2 = make_float2(sum_q, sum_q);
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float sc[32];
+          auto load = [&](int half) {
             tmem_ld16(lanes + s_col(x, buf) + 32 * half, reinterpret_cast<uint32_t *>(sc));
             tmem_ld16(lanes + s_col(x, buf) + 32 * half + 16, reinterpret_cast<uint32_t *>(sc + 16));
           };
-          auto mask = [&](int half, float *sc) {
+          float2 aa[16], cc[16];                     // of the scores that are on their way
+          auto terms = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float4 l = t_l[8 * half + i / 2], x0 = t_ab[16 * half + i], x1 = t_ab[16 * half + i + 1];
+              aa[i] = make_float2(x0.x, x0.y), aa[i + 1] = make_float2(x1.x, x1.y);
+              cc[i] = __ffma2_rn(make_float2(x0.z, x0.w), q2, make_float2(l.x, l.y)), cc[i + 1] = __ffma2_rn(make_float2(x1.z, x1.w), q2, make_float2(l.z, l.w));
+            }
+          };
+          auto scale = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 u = __ffma2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), aa[i], cc[i]);
+              sc[2 * i] = u.x, sc[2 * i + 1] = u.y;
+            }
             if (border) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
                 if (tok0 + 32 * half + i >= lim) sc[i] = -INFINITY;
             }
-          };
-          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          float s0[32], s1[32];
-          load(0, s0), load(1, s1);
-          tc_wait_ld();
-          mask(0, s0), mask(1, s1);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], fmaxf(s0[i], s1[i]));
-          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a;
+            for (int i = 0; i < 32; i += 2) m[(i >> 1) & 3] = fmaxf(m[(i >> 1) & 3], fmaxf(sc[i], sc[i + 1]));
+          };
+          load(1);
+          terms(1);
+          tc_wait_ld();
+          scale(1);
+          tmem_st16(lanes + s_col(x, buf) + 32, reinterpret_cast<const uint32_t *>(sc));
+          tmem_st16(lanes + s_col(x, buf) + 48, reinterpret_cast<const uint32_t *>(sc + 16));
+          load(0);
+          terms(0);
+          tc_wait_ld();
+          scale(0);
+          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
           if (__any_sync(0xffffffffu, most > top + kGrow)) {
-            const float now = fmaxf(most, top), f = ex2(top - now);
-            top = now, den *= f;
+            const float now = fmaxf(most - kUp, top), f = ex2(top - now);
+            top = now, den *= f, off *= f;
             if (j > 0) {
               wait(kODone + 2 * x + (buf ^ 1), ((g - 1) >> 1) & 1);
               tc_fence_after();
@@ -257,25 +294,35 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
               }
             }
           }
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          const float2 aa = make_float2(a, a), off = make_float2(-top, -top);
-          load(1, s1);                               // (on its way under the first half's exponentials)
-          auto weigh = [&](int half, const float *sc) {
+          float2 d2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, o2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 minus = make_float2(-top, -top);
+          float4 vms[16];
+          auto ahead = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) vms[i] = t_vm[16 * half + i];
+          };
+          auto weigh = [&](int half) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float2 e = __ffma2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), aa, off), w2 = make_float2(ex2(e.x), ex2(e.y));
-              sum[i & 1] = __fadd2_rn(sum[i & 1], w2);
-              w[i] = pack_h2(w2.x, w2.y);
+              const float4 vm = vms[i];
+              const float2 e = __fadd2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), minus), y2 = make_float2(ex2(e.x), ex2(e.y));
+              w[i] = pack_h2(y2.x, y2.y);
+              const float2 x2 = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));   // (the sums are those of the rounded weights, as in attend.cu)
+              d2[i & 1] = __ffma2_rn(x2, make_float2(vm.x, vm.y), d2[i & 1]);
+              o2[i & 1] = __ffma2_rn(x2, make_float2(vm.z, vm.w), o2[i & 1]);
             }
             // the weights over scores that have been read: sixteen columns hold 32 of them
             tmem_st16(lanes + s_col(x, buf) + 16 * half, w);
           };
-          weigh(0, s0);
+          ahead(0);
+          weigh(0);
+          tc_wait_st();                              // (the second half's u)
+          load(1);
+          ahead(1);
           tc_wait_ld();
-          mask(1, s1);
-          weigh(1, s1);
-          den += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          weigh(1);
+          den += (d2[0].x + d2[0].y) + (d2[1].x + d2[1].y), off += (o2[0].x + o2[0].y) + (o2[1].x + o2[1].y);
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -284,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         wait(kODone + 2 * x + ((g - 1) & 1), ((g - 1) >> 1) & 1);
         tc_fence_after();
       }
+      all += max(sg.count, 0);
       // ---- the rows, or this CTA's part of them
       const int from = n - left - sg.chunk0;
       if (active) {
@@ -321,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
           __syncwarp();
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<float4 *>(stage + 128 * lane + (((e / 4) ^ (lane & 7)) << 4)) = make_float4(o[e] * f, o[e + 1] * f, o[e + 2] * f, o[e + 3] * f);
+            *reinterpret_cast<float4 *>(stage + 128 * lane + (((e / 4) ^ (lane & 7)) << 4)) = make_float4((o[e] + off) * f, (o[e + 1] + off) * f, (o[e + 2] + off) * f, (o[e + 3] + off) * f);
           __syncwarp();
           if (!sg.whole) {
             float *const part = sums + (lane / 8 - lane) * kHd + ch + 4 * (lane & 7);
@@ -363,8 +411,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
       left -= take, cur.chunk += take;
     }
   } else if (warp < kWorkers + kMakers) {
-    // ================================================================ keys or values from codes: a block of sixteen tokens per warp
-    const int blk = (warp - kWorkers) & 3, value = (warp - kWorkers) >> 2, r = lane >> 2, c = lane & 3;
+    reg_dec<kRegsMaker>();
+    // ================================================================ keys, then values from codes: a block of sixteen tokens per warp
+    const int blk = warp - kWorkers;
     // where stmatrix puts the four pieces of a step: this lane names row lane & 7 of piece lane >> 3
     const int h1 = (lane >> 3) & 1, h2 = lane >> 4;
     uint32_t g = 0;
@@ -377,23 +426,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
         const uint32_t from = base + C::kOffRaw + raw * C::kRawBytes + blk * kBlockBytes;
         const int tok0 = (sg.chunk0 + j) * kTokens + blk * kKvBlock;
         wait(kRawFull + raw, (g / C::kRaw) & 1);
-        if (g >= (uint32_t)C::kKv) wait((value ? kVFree : kKFree) + st, (g / C::kKv - 1) & 1);
-        // scale and least value; zeros behind the last token, whatever lies there.  (A group that reaches to the end of fp16 may pass it with its greatest code: the
-        // scale is a step smaller then.)
-        auto pair = [&](uint32_t at, int tok) {
-          uint32_t v = lds32(at);
-          const float2 f = __half22float2(*reinterpret_cast<__half2 *>(&v));
-          if (__fmaf_rn(f.x, kBits == 4 ? 15.f : 255.f, f.y) > 65504.f) v -= 1;
-          return tok < cur.s.len ? v : 0u;
-        };
         constexpr int kPairs = 2 * kv_code_bytes(kHd, kBits);
-        {
-          uint32_t sc[2], lo[2];                     // keys: of tokens r and r + 8, twice each; values: of tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int t = value ? 8 * h + 2 * c : 8 * h + r;
-            const uint32_t u = pair(from + kPairs + 64 * value + 4 * t, tok0 + t), v = value ? pair(from + kPairs + 64 * value + 4 * t + 4, tok0 + t + 1) : u;
-            sc[h] = __byte_perm(u, v, 0x5410), lo[h] = __byte_perm(u, v, 0x7632);
+        constexpr float kMid = kBits == 4 ? 8.f : 128.f;
+        auto make = [&](auto kind) {
+          constexpr bool value = decltype(kind)::value;
+          if (g >= (uint32_t)C::kKv) wait((value ? kVFree : kKFree) + st, (g / C::kKv - 1) & 1);
+          if (value && lane < kKvBlock) {
+            // what the pairs of this token come to; whatever lies behind the last one is finite
+            const int t = kKvBlock * blk + lane;
+            uint32_t kp = lds32(from + kPairs + 4 * lane), vp = lds32(from + kPairs + 64 + 4 * lane);
+            if (tok0 + lane >= cur.s.len) kp = vp = 1u;
+            const float2 kf = __half22float2(*reinterpret_cast<__half2 *>(&kp)), vf = __half22float2(*reinterpret_cast<__half2 *>(&vp));
+            const float l = lg2(vf.x), vi = ex2(-l);   // log2(s) and 1 / s as that has it
+            float *const terms = reinterpret_cast<float *>(smem + C::kOffTerms + st * kTermBytes);
+            float *const ab = terms + 4 * (t / 2) + (t & 1), *const vm = ab + 2 * kTokens;
+            ab[0] = kf.x * p.scale_log2, ab[2] = __fmaf_rn(kf.x, kMid, kf.y) * p.scale_log2;
+            vm[0] = vi, vm[2] = __fmaf_rn(vf.y, vi, kMid);
+            terms[4 * kTokens + t] = l;
           }
           uint32_t to;                               // of step 0; keys advance by two 16-byte pieces of a row, values by sixteen rows
           if (value) to = base + C::kOffV + st * C::kVBytes + 128 * (8 * h1 + (lane & 7)) + (((2 * blk + h2) ^ (lane & 7)) << 4);
@@ -405,125 +454,127 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
 #pragma unroll
             for (int e = 0; e < (kBits == 4 ? 4 : 2); ++e) {
               const int k = (kBits == 4 ? 4 : 2) * i + e;
-              uint32_t f[4];                         // codes; pieces in the order (row half, k half) = (0, 0), (1, 0), (0, 1), (1, 1)
+              uint32_t f[4];                         // codes less the middle; pieces in the order (row half, k half) = (0, 0), (1, 0), (0, 1), (1, 1)
               if (kBits == 4) {
-                constexpr uint32_t kOne = 0x3c003c00u, kSixteenth = 0x2c002c00u, kLow = 0xe400e400u, kHigh = 0xd400d400u;   // -1024, -64
+                constexpr uint32_t kOne = 0x3c003c00u, kSixteenth = 0x2c002c00u, kLow = 0xe408e408u, kHigh = 0xd480d480u;   // -1032, -72
                 const uint32_t u = w[e], v = u >> 8;
                 const uint32_t n0 = h2_fma(lop_and_or(u, 0x000f000fu, 0x64006400u), kOne, kLow), n1 = h2_fma(lop_and_or(u, 0x00f000f0u, 0x64006400u), kSixteenth, kHigh);
                 const uint32_t n2 = h2_fma(lop_and_or(v, 0x000f000fu, 0x64006400u), kOne, kLow), n3 = h2_fma(lop_and_or(v, 0x00f000f0u, 0x64006400u), kSixteenth, kHigh);
                 f[0] = n0, f[1] = value ? n1 : n2, f[2] = value ? n2 : n1, f[3] = n3;
               } else {
-                constexpr uint32_t kOne = 0x3c003c00u, kMid = 0xe400e400u;
+                constexpr uint32_t kOne = 0x3c003c00u, kMiddle = 0xe480e480u;   // -1152
                 const uint32_t u = w[2 * e], v = w[2 * e + 1];
-                f[0] = h2_fma(__byte_perm(u, 0x64646464u, 0x4140), kOne, kMid), f[1] = h2_fma(__byte_perm(v, 0x64646464u, 0x4140), kOne, kMid);
-                f[2] = h2_fma(__byte_perm(u, 0x64646464u, 0x4342), kOne, kMid), f[3] = h2_fma(__byte_perm(v, 0x64646464u, 0x4342), kOne, kMid);
+                f[0] = h2_fma(__byte_perm(u, 0x64646464u, 0x4140), kOne, kMiddle), f[1] = h2_fma(__byte_perm(v, 0x64646464u, 0x4140), kOne, kMiddle);
+                f[2] = h2_fma(__byte_perm(u, 0x64646464u, 0x4342), kOne, kMiddle), f[3] = h2_fma(__byte_perm(v, 0x64646464u, 0x4342), kOne, kMiddle);
               }
-              // keys: rows are tokens, values: k is
-              f[0] = h2_fma(f[0], sc[0], lo[0]), f[1] = h2_fma(f[1], sc[value ? 0 : 1], lo[value ? 0 : 1]);
-              f[2] = h2_fma(f[2], sc[value ? 1 : 0], lo[value ? 1 : 0]), f[3] = h2_fma(f[3], sc[1], lo[1]);
               if (value) stmatrix4(to + 2048 * k, f);
               else stmatrix4(to + (k / 4) * (128 * kTokens) + ((((2 * k + h2) & 7) ^ (lane & 7)) << 4), f);
             }
           }
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar((value ? kVFull : kKFull) + st));
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar((value ? kVFull : kKFull) + st));
+        };
+        make(std::false_type{});
+        make(std::true_type{});
         if (lane == 0 && !lost) mbar_arrive(bar(kRawEmpty + raw));   // (a slot whose copy was given up on is not filled again)
       }
       left -= take, cur.chunk += take;
     }
-  } else if (warp < kIssuers + 2) {
-    // ================================================================ MMAs.  Everything that addresses them is the same in all lanes, and the compiler can see it (what came
-    // from memory by way of a shuffle): it then lies in uniform registers.  A warp per tile: one warp for both leaves the tensor core idle in each of its waits, which take 100 to 200
-    // cycles also when there is nothing to wait for (1.41 us per chunk of two tiles).
-    constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
-    const uint32_t ubase = __shfl_sync(0xffffffffu, base, 0), ubars = ubase + C::kOffBars;
-    const uint64_t q_desc = make_b_desc(ubase + (warp - kIssuers) * C::kQBytes), k_desc = make_b_desc(ubase + C::kOffK), v_desc = make_b_desc(ubase + C::kOffV);
-    constexpr uint32_t kQHalf16 = 8 * kTile, kK16 = C::kKBytes / 16, kKHalf16 = 8 * kTokens, kV16 = C::kVBytes / 16;
-    auto ubar = [&](int i) { return ubars + 8 * i; };
-    const int x = warp - kIssuers;
-    int k_at = 0, v_at = 0;                          // slots of the next keys and values ...
-    uint32_t k_turn = 0, v_turn = 0;                 // ... and the parity of their barriers
-    uint32_t scored = 0, weighed = 0, tiles = 0;     // chunks whose scores, whose products have been issued; tiles of queries
-    // scores of the next chunk.  (A second tile without rows lets go of the keys and values all the same, when they are there: their barriers count two arrivals.)
-    auto scores = [&](bool active) {
-      spin(kKFull + k_at, k_turn);
-      if (active) {
-        tc_fence_after();
-        if (!lost) {
-#pragma unroll
-          for (int h = 0; h < C::kHalves; ++h)
-            mma4_ss(tmem + s_col(x, scored & 1), q_desc + h * kQHalf16, k_desc + (uint64_t)(k_at * kK16 + h * kKHalf16), idesc_s, h);
-        }
-        tc_commit(ubar(kSFull + 2 * x + (scored & 1)));
-        ++scored;
-      }
-      tc_commit(ubar(kKFree + k_at));
-      if (++k_at == C::kKv) k_at = 0, k_turn ^= 1;
-    };
-    for (int left = __shfl_sync(0xffffffffu, n, 0); left > 0;) {
-      settle<kRows, kTokens>(p, cur);
-      const Segment sg = segment(p, cur, left);
-      const int take = __shfl_sync(0xffffffffu, min(left, cur.s.chunks - cur.chunk), 0);
-      const int count = __shfl_sync(0xffffffffu, sg.count, 0);
-      const bool active = __shfl_sync(0xffffffffu, sg.rows > kTile * x, 0);
-      if (count > 0) {
-        if (active) spin(kQFull + x, tiles++ & 1);
-        scores(active);
-        for (int j = 0; j < count; ++j) {
-          if (j + 1 < count) scores(active);
-          spin(kVFull + v_at, v_turn);
-          if (active) {
-            spin(kPFull + 2 * x + (weighed & 1), (weighed >> 1) & 1);
-            tc_fence_after();
-            if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, weighed & 1), v_desc + (uint64_t)(v_at * kV16), idesc_o, j > 0);
-            tc_commit(ubar(kODone + 2 * x + (weighed & 1)));
-            ++weighed;
-          }
-          tc_commit(ubar(kVFree + v_at));
-          if (++v_at == C::kKv) v_at = 0, v_turn ^= 1;
-        }
-      }
-      left -= take, cur.chunk += take;
-    }
-    // everything issued is over before the tensor memory is given back, whatever was waited for
-    tc_commit(bar(kDone + x));
-    for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kDone + x), 0); ++i) __nanosleep(100);
   } else {
-    // ================================================================ copies: lane i brings block i of the chunk; its page is looked up a chunk ahead
-    uint32_t g = 0;
-    const uint64_t keep = policy_evict_first();
-    const int run = min(1 << p.kv.page_shift, kBlocks);   // blocks next to each other: one copy, by the lane of the first one
-    int block = 0, blocks = 0, page = 0;
-    const uint8_t *heads = nullptr;
-    auto look_up = [&](const Segment &sg, int j) {
-      block = (sg.chunk0 + j) * kBlocks, blocks = min(kBlocks, (cur.s.len + kKvBlock - 1) / kKvBlock - block);
-      heads = p.kv.pages + ((long long)sg.head << p.kv.page_shift) * kBlockBytes;
-      page = lane < blocks && lane % run == 0 ? kv_page(p.kv, p.b, cur.seq, block + lane) : 0;
-    };
-    for (int left = n; left > 0;) {
-      settle<kRows, kTokens>(p, cur);
-      const Segment sg = segment(p, cur, left);
-      const int take = min(left, cur.s.chunks - cur.chunk);
-      if (sg.count > 0) look_up(sg, 0);
-      for (int j = 0; j < sg.count && !lost; ++j, ++g) {
-        const int raw = g % C::kRaw;
-        if (g >= (uint32_t)C::kRaw) wait(kRawEmpty + raw, (g / C::kRaw - 1) & 1);
-        if (lost) break;
-        if (lane == 0) mbar_arrive_expect_tx(bar(kRawFull + raw), blocks * kBlockBytes);
-        __syncwarp();
-        if (page < 0) kv_report(p.status), page = 0;         // (the first page of the cache in its place)
-        if (lane < blocks && lane % run == 0)
-          bulk_copy_g2s_hint(base + C::kOffRaw + raw * C::kRawBytes + lane * kBlockBytes, heads + kv_offset(p.kv, page, block + lane, kBlockBytes),
-                             min(run, blocks - lane) * kBlockBytes, bar(kRawFull + raw), keep);
-        if (j + 1 < sg.count) look_up(sg, j + 1);
+    reg_dec<kRegsRest>();                            // (one instruction for the whole warpgroup)
+    if (warp < kIssuers + 2) {
+      // ================================================================ MMAs.  Everything that addresses them is the same in all lanes, and the compiler can see it (what came
+      // from memory by way of a shuffle): it then lies in uniform registers.  A warp per tile: one warp for both leaves the tensor core idle in each of its waits, which take 100 to 200
+      // cycles also when there is nothing to wait for (1.41 us per chunk of two tiles).
+      constexpr uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTokens >> 3) << 17) | (8u << 24), idesc_o = (1u << 4) | ((uint32_t)(kHd >> 3) << 17) | (8u << 24);
+      const uint32_t ubase = __shfl_sync(0xffffffffu, base, 0), ubars = ubase + C::kOffBars;
+      const uint64_t q_desc = make_b_desc(ubase + (warp - kIssuers) * C::kQBytes), k_desc = make_b_desc(ubase + C::kOffK), v_desc = make_b_desc(ubase + C::kOffV);
+      constexpr uint32_t kQHalf16 = 8 * kTile, kK16 = C::kKBytes / 16, kKHalf16 = 8 * kTokens, kV16 = C::kVBytes / 16;
+      auto ubar = [&](int i) { return ubars + 8 * i; };
+      const int x = warp - kIssuers;
+      int k_at = 0, v_at = 0;                          // slots of the next keys and values ...
+      uint32_t k_turn = 0, v_turn = 0;                 // ... and the parity of their barriers
+      uint32_t scored = 0, weighed = 0, tiles = 0;     // chunks whose scores, whose products have been issued; tiles of queries
+      // scores of the next chunk.  (A second tile without rows lets go of the keys and values all the same, when they are there: their barriers count two arrivals.)
+      auto scores = [&](bool active) {
+        spin(kKFull + k_at, k_turn);
+        if (active) {
+          tc_fence_after();
+          if (!lost) {
+#pragma unroll
+            for (int h = 0; h < C::kHalves; ++h)
+              mma4_ss(tmem + s_col(x, scored & 1), q_desc + h * kQHalf16, k_desc + (uint64_t)(k_at * kK16 + h * kKHalf16), idesc_s, h);
+          }
+          tc_commit(ubar(kSFull + 2 * x + (scored & 1)));
+          ++scored;
+        }
+        tc_commit(ubar(kKFree + k_at));
+        if (++k_at == C::kKv) k_at = 0, k_turn ^= 1;
+      };
+      for (int left = __shfl_sync(0xffffffffu, n, 0); left > 0;) {
+        settle<kRows, kTokens>(p, cur);
+        const Segment sg = segment(p, cur, left);
+        const int take = __shfl_sync(0xffffffffu, min(left, cur.s.chunks - cur.chunk), 0);
+        const int count = __shfl_sync(0xffffffffu, sg.count, 0);
+        const bool active = __shfl_sync(0xffffffffu, sg.rows > kTile * x, 0);
+        if (count > 0) {
+          if (active) spin(kQFull + x, tiles++ & 1);
+          scores(active);
+          for (int j = 0; j < count; ++j) {
+            if (j + 1 < count) scores(active);
+            spin(kVFull + v_at, v_turn);
+            if (active) {
+              spin(kPFull + 2 * x + (weighed & 1), (weighed >> 1) & 1);
+              tc_fence_after();
+              if (!lost) mma4_ts(tmem + o_col(x), tmem + s_col(x, weighed & 1), v_desc + (uint64_t)(v_at * kV16), idesc_o, j > 0);
+              tc_commit(ubar(kODone + 2 * x + (weighed & 1)));
+              ++weighed;
+            }
+            tc_commit(ubar(kVFree + v_at));
+            if (++v_at == C::kKv) v_at = 0, v_turn ^= 1;
+          }
+        }
+        left -= take, cur.chunk += take;
       }
-      left -= take, cur.chunk += take;
+      // everything issued is over before the tensor memory is given back, whatever was waited for
+      tc_commit(bar(kDone + x));
+      for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kDone + x), 0); ++i) __nanosleep(100);
+    } else if (warp == kIssuers + 2) {
+      // ================================================================ copies: lane i brings block i of the chunk; its page is looked up a chunk ahead
+      uint32_t g = 0;
+      const uint64_t keep = policy_evict_first();
+      const int run = min(1 << p.kv.page_shift, kBlocks);   // blocks next to each other: one copy, by the lane of the first one
+      int block = 0, blocks = 0, page = 0;
+      const uint8_t *heads = nullptr;
+      auto look_up = [&](const Segment &sg, int j) {
+        block = (sg.chunk0 + j) * kBlocks, blocks = min(kBlocks, (cur.s.len + kKvBlock - 1) / kKvBlock - block);
+        heads = p.kv.pages + ((long long)sg.head << p.kv.page_shift) * kBlockBytes;
+        page = lane < blocks && lane % run == 0 ? kv_page(p.kv, p.b, cur.seq, block + lane) : 0;
+      };
+      for (int left = n; left > 0;) {
+        settle<kRows, kTokens>(p, cur);
+        const Segment sg = segment(p, cur, left);
+        const int take = min(left, cur.s.chunks - cur.chunk);
+        if (sg.count > 0) look_up(sg, 0);
+        for (int j = 0; j < sg.count && !lost; ++j, ++g) {
+          const int raw = g % C::kRaw;
+          if (g >= (uint32_t)C::kRaw) wait(kRawEmpty + raw, (g / C::kRaw - 1) & 1);
+          if (lost) break;
+          if (lane == 0) mbar_arrive_expect_tx(bar(kRawFull + raw), blocks * kBlockBytes);
+          __syncwarp();
+          if (page < 0) kv_report(p.status), page = 0;         // (the first page of the cache in its place)
+          if (lane < blocks && lane % run == 0)
+            bulk_copy_g2s_hint(base + C::kOffRaw + raw * C::kRawBytes + lane * kBlockBytes, heads + kv_offset(p.kv, page, block + lane, kBlockBytes),
+                               min(run, blocks - lane) * kBlockBytes, bar(kRawFull + raw), keep);
+          if (j + 1 < sg.count) look_up(sg, j + 1);
+        }
+        left -= take, cur.chunk += take;
+      }
+      // the CTA outlasts its copies, also when nobody waits for them any more
+      for (uint32_t k = g < (uint32_t)C::kRaw ? 0 : g - C::kRaw; k < g; ++k)
+        for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) __nanosleep(100);
     }
-    // the CTA outlasts its copies, also when nobody waits for them any more
-    for (uint32_t k = g < (uint32_t)C::kRaw ? 0 : g - C::kRaw; k < g; ++k)
-      for (int i = 0; i < 1 << 20 && !mbar_test_wait(bar(kRawFull + k % C::kRaw), (k / C::kRaw) & 1); ++i) __nanosleep(100);
   }
   __syncthreads();
   if (warp == kIssuers) tmem_dealloc<512>(tmem);
@@ -556,6 +607,11 @@ int launch(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   if (ready == 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) != cudaSuccess) {
     (void)cudaGetLastError();
     return ROSAQ_ERR_CUDA;
+  }
+  cudaFuncAttributes attr{};
+  if (ready == 0 && (cudaFuncGetAttributes(&attr, kern) != cudaSuccess || attr.numRegs * 4 < 2 * kRegsSoftmax + kRegsMaker + kRegsRest)) {
+    (void)cudaGetLastError();
+    return ROSAQ_ERR_CUDA;                           // (the warpgroups would wait for registers that the block does not have)
   }
   ready = 1;
   const int ctas = std::min(ctx->sm_count, kAtMaxCtas);

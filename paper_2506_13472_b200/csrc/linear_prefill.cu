@@ -134,14 +134,6 @@ __device__ __forceinline__ unsigned pf_ld_relaxed(const unsigned *ptr) {
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(ptr) : "memory");
   return v;
 }
-template <int kRegs>
-__device__ __forceinline__ void reg_dec() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-template <int kRegs>
-__device__ __forceinline__ void reg_inc() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
 // The fp16 tile of an operand (16-byte chunks of eight channels, column by column) is a K-major operand without swizzle:
 // eight columns 128 bytes apart from the next eight, the next eight channels kTileN * 16 bytes further.
 __device__ __forceinline__ uint64_t make_a_desc(uint32_t smem_addr) {

@@ -246,6 +246,16 @@ __device__ __forceinline__ uint32_t h2_sub_mul(uint32_t v, uint32_t sub, uint32_
   return *reinterpret_cast<uint32_t *>(&r);
 }
 
+// Registers per thread of the four warps of a warpgroup.  What one group takes on the others have to have given up, of what the block was launched with.
+template <int kRegs>
+__device__ __forceinline__ void reg_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void reg_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+
 // K-major, 128-byte-swizzled shared-memory operand: 8-row groups 1024 bytes apart.
 __device__ __forceinline__ uint64_t make_b_desc(uint32_t smem_addr) {
   return (uint64_t)((smem_addr >> 4) & 0x3fff) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);

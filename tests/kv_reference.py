@@ -98,16 +98,14 @@ def values(pages_tensor, heads, hd, bits, page, table, n):
     return out
 
 
-def attention(q, kv, seen, scale, rounded=False):
+def attention(q, kv, seen, scale):
     """(out, bound) of query rows q [n][hq][hd] (float64) over kv = values(...) of all tokens, row i seeing the tokens where seen[i] is true.
 
     bound, element by element: half a step of the fp16 result, and in units of A + B with A = sum p s d / sum p, B = sum p |lo| / sum p
       2^-11                    the weight's rounding to fp16
       (tokens / 16 + 64) 2^-23 one accumulator update per 16 tokens (the tensor core truncates), and the joining of partial sums
       2^-20 m                  scores: fp32 sums of terms up to m = scale (|q| s c + |sum q| |lo|), a few roundings, and the exponential
-    and 2^-25 of the greatest weight per token, for weights that fp16 holds as subnormal numbers.
-    rounded: keys and values are rounded to fp16 first (many query rows): half a step of each value more, 2^-11 (A + B), and scores off by 2^-11 k with
-    k = scale |q| |key|, which moves the weights and their sum."""
+    and 2^-25 of the greatest weight per token, for weights that fp16 holds as subnormal numbers."""
     (kc, kl, _), (vc, vl, vs) = kv
     n, hq, hd = q.shape
     g = hq // kc.shape[1]
@@ -131,10 +129,6 @@ def attention(q, kv, seen, scale, rounded=False):
     tokens = k.shape[0]
     small = tokens * 2.0 ** -25 * (p * rep(vs)[..., 0].T[None]).amax(-1, keepdim=True) * vc.div(vs.clamp(min=1e-30)).amax() / den
     bound = 2.0 ** -11 * out.abs() + 2.0 ** -25 + (2.0 ** -11 + (tokens / 16 + 64) * 2.0 ** -23 + 2.0 ** -20 * (1 + m)) * (a + b) + small
-    if rounded:
-        mk = torch.einsum("nhd,thd->nht", q.abs(), k.abs()) * abs(scale)
-        mk = torch.where(seen[:, None, :], mk, torch.zeros_like(mk)).amax(-1, keepdim=True)
-        bound = bound + (2.0 ** -11 + 2 * 2.0 ** -11 * mk) * (a + b)
     return torch.where(any_seen, out, torch.zeros_like(out)), bound
 
 

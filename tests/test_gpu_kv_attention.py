@@ -207,10 +207,6 @@ def fill(ctx, rng, held, table, lens, loud=1.0, v_size=1.0, offset=0.0):
 
 def expect(held, table, lens, new, q, scale, prefix=None):
     """(out, bound) of all rows."""
-    group = q.shape[1] // held.width
-    # the kernel that rounds keys and values to fp16
-    many = lambda rows, seqs, room: rows * group >= 64 and rows * group * seqs * held.n_kv_heads * room >= 1 << 22  # noqa: E731
-    rounded = many(-(-q.shape[0] // len(lens)), len(lens), table.shape[1] * held.page_tokens) or (prefix is not None and many(q.shape[0], 1, prefix[1]))
     outs, bounds, at = [], [], 0
     hd, hq = held.head_dim, q.shape[1] // held.head_dim
     args = (held.pages, held.n_kv_heads, hd, held.bits, held.page_tokens)
@@ -222,7 +218,7 @@ def expect(held, table, lens, new, q, scale, prefix=None):
         if pre:
             kv = [[torch.cat([a, b]) for a, b in zip(x, y)] for x, y in zip(pre, kv)]
         seen = torch.arange(np_ + n, device="cuda")[None, :] < np_ + n - m + 1 + torch.arange(m, device="cuda")[:, None]
-        o, b = ref.attention(q[at:at + m].double().view(m, hq, hd), kv, seen, scale, rounded)
+        o, b = ref.attention(q[at:at + m].double().view(m, hq, hd), kv, seen, scale)
         outs.append(o.reshape(m, -1)), bounds.append(b.reshape(m, -1))
         at += m
     return torch.cat(outs), torch.cat(bounds)
