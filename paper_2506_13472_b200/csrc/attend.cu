@@ -3,7 +3,7 @@
 // With k = lo_k + s_k c and v = lo_v + s_v d (codes c, d; one pair (s, lo) per token) the sums split into products of codes and sums over tokens:
 //   q . k = s_k (q . c) + lo_k sum(q),      sum_t p_t v_t = sum_t (p_t s_t) d_t + sum_t p_t lo_t.
 // So no key is dequantised: nibbles and bytes, masked out of their words, ARE fp16 numbers (subnormal: code * 2^-24), exact operands of the
-// tensor core.  Value codes are taken about the middle of their range, d_t - 2^(bits - 1), which costs an addition per pair and keeps the sums as small as
+// tensor core.  Value codes are taken about the middle of their range, d_t - 10 or d_t - 128, which costs an addition per pair and keeps the sums as small as
 // the result: of positive codes the roundings of the weights and of the accumulators would all point one way (against 64 bits, 26000 tokens
 // at 8 bits: 1.2e-3 that way).  The weights of the second product keep their size whatever that of the values: u_t = score_t log2(e) + log2(s_t) is what the
 // running maximum is taken of, so that p_t s_t has its greatest value between 2^10 and 2^15 before the rounding to fp16 (2^-11 relative, 2^-35 of the
@@ -12,8 +12,8 @@
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
 //
-// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, 455 per pair
-// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 132 us, 119 without the
+// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 480 per pair
+// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 135 us, 119 without the
 // arithmetic, 95 at the copy bandwidth.  Short calls are bound by latency: 5.7 us for one chunk, 0.9 to 1.0 us per further chunk of a warp, 5 us to join CTAs.
 // The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the device, so a captured launch
 // follows them.  A CTA's share is cut into one run per warp, each with slots of its own, all filled by one more warp, a lane per slot (warps that fill their own: 153 to 168 us
@@ -28,10 +28,10 @@ namespace {
 
 constexpr int kChunk = 2, kTokens = kChunk * kKvBlock;   // blocks that a warp takes at a time
 constexpr int kRows = 8;                            // query rows of a tile
-// From kManyRows query rows per sequence and key/value head on, and from kManyWork of (row, key/value head, token that the table has room for) in all: attend_rows.cu, which takes 9 us
+// From kManyRows query rows per sequence and key/value head on, and from kManyWork of (row, key/value head, token that the table has room for) in all: attend_rows.cu, which takes 10 us
 // more for any call and a third to a half of the time per row and token.  (us here and there, 32 query and 8 key/value heads of 128 at 4 bits: 32 rows of each of 16 sequences of 1000
-// tokens 35 and 38, 64 rows 48 and 39; of one sequence of 500 tokens 64 rows 12.5 and 22; of 4000 tokens 64 rows 26 and 31, 128 rows 33 and 31; of 30000 tokens 64 rows 65 and 52;
-// 128 rows behind a prefix of 500 tokens 21 and 31, of 4000 41 and 39, of 16000 76 and 49.)
+// tokens 34 and 35, 64 rows 47 and 37; of one sequence of 500 tokens 64 rows 12 and 24; of 4000 tokens 64 rows 26 and 25, 128 rows 32 and 26; of 30000 tokens 64 rows 65 and 50;
+// 128 rows behind a prefix of 500 tokens 21 and 32, of 4000 40 and 36, of 16000 76 and 46.)
 constexpr long long kManyRows = 64, kManyWork = 1ll << 22;
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 }
 // A fragment of step j of a block, keys (token, channel) or values (channel, token), in units of 2^-24: the codes; at four bits sixteen times the codes of the second nibbles, which
 // are channels 8-15.  (Values: whole bytes in the rows of channels 0-7, what is too much taken off at the end, are an operation less per word; but what the accumulators cut off
-// is relative to the sixteenfold sum then: 131071 tokens 3.2e-4 off instead of 2.x.)
+// is relative to the sixteenfold sum then: 131071 tokens 3.5e-4 off, 3.2e-4 so.)
 template <int kBits, bool kValue>
 __device__ __forceinline__ void code_fragment(const uint32_t *w, int j, uint32_t *a) {
   if (kBits == 4) {
@@ -245,6 +245,10 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
     // Value codes about the middle of their range: the sums of the weights, as the tensor core has them, times minus the middle gather in `low` (one MMA per block), and every
     // kFlush chunks they are added to the accumulators.
     constexpr int kFlush = 4;
+    // (The tensor core cuts off the sums' last bits.  What it cuts off the codes' sums and off the middle's goes the other way, and cancels when the middle has about as many zeros at
+    // its end as codes have: else all parts of a long context are off to one side.  131000 tokens at 4 bits: signed error -1.7e-4 with 8, +9e-5 with 7, below 3e-5 with 6 and 10.)
+    constexpr float kMiddle = kBits == 4 ? 10.f : 128.f;
+    constexpr uint32_t kLow = kBits == 4 ? 0x800a800au : 0x80808080u, kHigh = kBits == 4 ? 0x80a080a0u : 0x80808080u;   // minus that times 2^-24, and times 2^-20
     float low[4] = {0.f, 0.f, 0.f, 0.f};
     auto take_off = [&]() {
 #pragma unroll
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
           const float2 kf = __half22float2(*reinterpret_cast<__half2 *>(&kp)), vf = __half22float2(*reinterpret_cast<__half2 *>(&vp));
           const float lv = lg2(vf.x), vi = ex2(-lv);   // log2(s) and 1 / s as that has it
           terms[lane] = make_float4(kf.x * key_scale, kf.y, lv, vi);
-          term_vl[lane] = __fmaf_rn(vf.y, vi, kBits == 4 ? 8.f : 128.f);   // (lo + s 2^(bits - 1)) / s
+          term_vl[lane] = __fmaf_rn(vf.y, vi, kMiddle);   // (lo + s middle) / s
           __syncwarp();
         }
         const uint32_t at = base + 16 * lane;
@@ -361,8 +365,8 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
             pf[b][h] = transpose8(w);
           }
         }
-        // minus the middle of what the fragments hold: 8 and 16 * 8, or 128
-        const uint32_t mid[4] = {kBits == 4 ? 0x80088008u : 0x80808080u, 0x80808080u, kBits == 4 ? 0x80088008u : 0x80808080u, 0x80808080u};
+        // minus the middle of the codes, as the fragments have them
+        const uint32_t mid[4] = {kLow, kHigh, kLow, kHigh};
 #pragma unroll
         for (int b = 0; b < kChunk; ++b) mma16816(low, mid, pf[b][0], pf[b][1]);
 #pragma unroll

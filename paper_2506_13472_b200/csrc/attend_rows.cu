@@ -4,14 +4,15 @@
 // accumulators in tensor memory.  C and D are the codes less the middle of their range (8 or 128), exact in fp16, so nothing but the softmax weights is rounded (2^-11), as in
 // attend.cu; with A = scale s_k, B = scale (lo_k + middle s_k), L = log2 s_v, M = lo_v / s_v + middle of a token (scale: with log2 e)
 //   u = A S + (B sum(q) + L),   p s_v = 2^(u - top),   out = (sum (p s_v) D + sum (p s_v) M) / sum (p s_v) / s_v.
-// (Keys and values rounded to fp16 instead need none of the terms: 1.25 us per chunk of 256 rows, and an error of 6.5e-4 where this has 2.8e-4 and the rounding of the result alone
+// (Keys and values rounded to fp16 instead need none of the terms: 1.25 us per chunk of 256 rows, and an error of 6.5e-4 where this has 2.7e-4 and the rounding of the result alone
 // 2.1e-4: some channels of keys are several times larger than others, and their roundings move the scores.)
 // A CTA has up to two tiles of 128 rows, which share the operands that four warps make of the codes, in the fragment order of the cache's words: one stmatrix stores four 8 x 8
 // pieces, rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  Softmax: a row per thread, four warps per
 // tile; the scores of the next chunk go to a second buffer.  What the weights of a row are relative to is seldom renewed: then its accumulators are rescaled in tensor memory.
 //
-// Measured: 1.65 us per chunk and pair of tiles (head of 128), 3100 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
-// channels 64), the exponentials 1024, the terms 2560 of the shared memory's bandwidth (20 bytes per row and token: a broadcast costs as much as any load).  Before the first chunk
+// Measured: 1.7 us per chunk and pair of tiles (head of 128), 3200 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
+// channels 64), the exponentials 1024, the terms 2560 of the shared memory's bandwidth (20 bytes per row and token: a broadcast costs as much as any load).  Softmax warps have 176
+// registers, so that terms are loaded while scores are on their way (all warps with 128: 1.78 us; a warp per tile that issues MMAs, as one for both leaves the tensor core idle).  Before the first chunk
 // and behind the last one about 8 us: the share, the queries and the first codes 4, the rows 4 (135 KB of partial sums per CTA).
 #include <algorithm>
 #include <type_traits>
