@@ -6,14 +6,14 @@
 // tensor core.  Value codes are taken about the middle of their range, d_t - 10 or d_t - 128, which costs an addition per pair and keeps the sums as small as
 // the result: of positive codes the roundings of the weights and of the accumulators would all point one way (against 64 bits, 26000 tokens
 // at 8 bits: 1.2e-3 that way).  The weights of the second product keep their size whatever that of the values: u_t = score_t log2(e) + log2(s_t) is what the
-// running maximum is taken of, so that p_t s_t has its greatest value between 2^10 and 2^15 before the rounding to fp16 (2^-11 relative, 2^-35 of the
-// greatest weight absolute), while sum(p_t) and sum(p_t lo_t) stay in fp32.
+// running maximum is taken of, so that p_t s_t has its greatest value between 2^10 and 2^15 and is cut to 11 bits, an fp16 number (2^-35 of
+// the greatest weight absolute), while sum(p_t) and sum(p_t lo_t) are in fp32, of the same weights.
 //
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
 //
-// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 480 per pair
-// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 135 us, 119 without the
+// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 490 per pair
+// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 136 us, 119 without the
 // arithmetic, 95 at the copy bandwidth.  Short calls are bound by latency: 5.7 us for one chunk, 0.9 to 1.0 us per further chunk of a warp, 5 us to join CTAs.
 // The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the device, so a captured launch
 // follows them.  A CTA's share is cut into one run per warp, each with slots of its own, all filled by one more warp, a lane per slot (warps that fill their own: 153 to 168 us
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
           uint32_t kp = lds32(at), vp = lds32(at + 64);
           if (tok0 + lane >= most_seen) kp = vp = 0x00000001u;   // whatever lies behind the last token
           const float2 kf = __half22float2(*reinterpret_cast<__half2 *>(&kp)), vf = __half22float2(*reinterpret_cast<__half2 *>(&vp));
-          const float lv = lg2(vf.x), vi = ex2(-lv);   // log2(s) and 1 / s as that has it
+          const float lv = lg2(fmaxf(vf.x, kLeastScale)), vi = ex2(-lv);   // log2(s) and 1 / s as that has it
           terms[lane] = make_float4(kf.x * key_scale, kf.y, lv, vi);
           term_vl[lane] = __fmaf_rn(vf.y, vi, kMiddle);   // (lo + s middle) / s
           __syncwarp();
@@ -357,12 +357,10 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
         for (int b = 0; b < kChunk; ++b) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            // (the sums are those of the rounded weights: where few tokens have all the weight, their roundings cancel)
-            const uint32_t w = pack_h2(ex2(sc[b][2 * h] - top[0]), ex2(sc[b][2 * h + 1] - top[1]));
-            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+            const float2 x = weights(sc[b][2 * h] - top[0], sc[b][2 * h + 1] - top[1]);
             den[0] = __fmaf_rn(x.x, vi[b][h], den[0]), den[1] = __fmaf_rn(x.y, vi[b][h], den[1]);
             off[0] = __fmaf_rn(x.x, vl[b][h], off[0]), off[1] = __fmaf_rn(x.y, vl[b][h], off[1]);
-            pf[b][h] = transpose8(w);
+            pf[b][h] = transpose8(pack_h2(x.x, x.y));
           }
         }
         // minus the middle of the codes, as the fragments have them

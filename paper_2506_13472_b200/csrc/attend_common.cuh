@@ -12,6 +12,7 @@ namespace rosaq {
 // pass 2^kGrow, which fp16 still holds.  A long context has most of its weight in tokens far below the greatest, and fp16 is subnormal from 2^-14 on (against 64 bits, 131071 tokens
 // at 4 bits: 3.5e-4 with a greatest weight of one).
 constexpr float kNone = -1e30f;                     // top of a row that has seen nothing
+constexpr float kLeastScale = 5.9604644775390625e-8f;   // of a value: what writing puts in the place of zero, which pages that were never written may hold
 constexpr float kUp = 10.f, kGrow = 15.f;
 
 struct AtParams {
@@ -58,6 +59,14 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Two weights: 2^x and 2^y rounded to 11 bits, which fp16 holds without rounding from 2^-14 on.  The sums of a row's weights take the same number, so that what all of them lose cancels, and what is
+// left is as little as rounding leaves (with sums of unrounded weights 131000 tokens at 4 bits were 3.6e-4 off instead of 2.8e-4).  Below 2^-14 only the product loses more:
+// weights of values next to nothing, whose scale is small, may vanish in fp16 and yet have most of the softmax.
+__device__ __forceinline__ float2 weights(float x, float y) {
+  // (Veltkamp's splitting: the upper 24 - 13 bits, to nearest; what is no number stays none)
+  const float2 w = make_float2(ex2(x), ex2(y)), g = __fmul2_rn(w, make_float2(8193.f, 8193.f));
+  return __fadd2_rn(g, __ffma2_rn(g, make_float2(-1.f, -1.f), w));
 }
 __device__ __forceinline__ float lg2(float x) {
   float y;

@@ -1,7 +1,7 @@
 // rosaq_attend for many query rows per sequence and key/value head: a prompt, or a batch behind a shared prefix.
 //
 // tcgen05: per chunk of 64 tokens S = Q C^T (128 rows x 64 tokens, both operands in shared memory) and O += P D (P in tensor memory over its scores, D in shared memory), fp32
-// accumulators in tensor memory.  C and D are the codes less the middle of their range (8 or 128), exact in fp16, so nothing but the softmax weights is rounded (2^-11), as in
+// accumulators in tensor memory.  C and D are the codes less the middle of their range (8 or 128), exact in fp16, so nothing but the softmax weights loses bits, as in
 // attend.cu; with A = scale s_k, B = scale (lo_k + middle s_k), L = log2 s_v, M = lo_v / s_v + middle of a token (scale: with log2 e)
 //   u = A S + (B sum(q) + L),   p s_v = 2^(u - top),   out = (sum (p s_v) D + sum (p s_v) M) / sum (p s_v) / s_v.
 // (Keys and values rounded to fp16 instead need none of the terms: 1.25 us per chunk of 256 rows, and an error of 6.5e-4 where this has 2.7e-4 and the rounding of the result alone
@@ -10,7 +10,7 @@
 // pieces, rows of keys (channels contiguous) and rows of channels of values (tokens contiguous), both K-major with the 128-byte swizzle.  Softmax: a row per thread, four warps per
 // tile; the scores of the next chunk go to a second buffer.  What the weights of a row are relative to is seldom renewed: then its accumulators are rescaled in tensor memory.
 //
-// Measured: 1.7 us per chunk and pair of tiles (head of 128), 3200 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
+// Measured: 1.75 us per chunk and pair of tiles (head of 128), 3300 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
 // channels 64), the exponentials 1024, the terms 2560 of the shared memory's bandwidth (20 bytes per row and token: a broadcast costs as much as any load).  Softmax warps have 176
 // registers, so that terms are loaded while scores are on their way (all warps with 128: 1.78 us; a warp per tile that issues MMAs, as one for both leaves the tensor core idle).  Before the first chunk
 // and behind the last one about 8 us: the share, the queries and the first codes 4, the rows 4 (135 KB of partial sums per CTA).
@@ -307,9 +307,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float4 vm = vms[i];
-              const float2 e = __fadd2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), minus), y2 = make_float2(ex2(e.x), ex2(e.y));
-              w[i] = pack_h2(y2.x, y2.y);
-              const float2 x2 = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));   // (the sums are those of the rounded weights, as in attend.cu)
+              const float2 e = __fadd2_rn(make_float2(sc[2 * i], sc[2 * i + 1]), minus), x2 = weights(e.x, e.y);
+              w[i] = pack_h2(x2.x, x2.y);
               d2[i & 1] = __ffma2_rn(x2, make_float2(vm.x, vm.y), d2[i & 1]);
               o2[i & 1] = __ffma2_rn(x2, make_float2(vm.z, vm.w), o2[i & 1]);
             }
@@ -438,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
             uint32_t kp = lds32(from + kPairs + 4 * lane), vp = lds32(from + kPairs + 64 + 4 * lane);
             if (tok0 + lane >= cur.s.len) kp = vp = 1u;
             const float2 kf = __half22float2(*reinterpret_cast<__half2 *>(&kp)), vf = __half22float2(*reinterpret_cast<__half2 *>(&vp));
-            const float l = lg2(vf.x), vi = ex2(-l);   // log2(s) and 1 / s as that has it
+            const float l = lg2(fmaxf(vf.x, kLeastScale)), vi = ex2(-l);   // log2(s) and 1 / s as that has it
             float *const terms = reinterpret_cast<float *>(smem + C::kOffTerms + st * kTermBytes);
             float *const ab = terms + 4 * (t / 2) + (t & 1), *const vm = ab + 2 * kTokens;
             ab[0] = kf.x * p.scale_log2, ab[2] = __fmaf_rn(kf.x, kMid, kf.y) * p.scale_log2;

@@ -102,7 +102,7 @@ def attention(q, kv, seen, scale):
     """(out, bound) of query rows q [n][hq][hd] (float64) over kv = values(...) of all tokens, row i seeing the tokens where seen[i] is true.
 
     bound, element by element: half a step of the fp16 result, and in units of A + B with A = sum p s d / sum p, B = sum p |lo| / sum p
-      2^-11                    the weight's rounding to fp16
+      2^-11                    the weights' 11 bits, each off by no more than that from a factor that all of a row share
       (tokens / 16 + 64) 2^-23 one accumulator update per 16 tokens (the tensor core truncates), and the joining of partial sums
       2^-20 m                  scores: fp32 sums of terms up to m = scale (|q| s c + |sum q| |lo|), a few roundings, and the exponential
     and 2^-25 of the greatest weight per token, for weights that fp16 holds as subnormal numbers."""

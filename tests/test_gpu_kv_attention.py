@@ -599,3 +599,35 @@ def test_many_rows_that_are_no_numbers(ctx):
     bad[1, 0] = bad[69, 1] = bad[139, 2] = True
     assert torch.equal(torch.isnan(got).any(-1), bad) and torch.equal(torch.isnan(got).all(-1), bad)
     inside(got[~bad], want.view(140, 4, 128)[~bad], bound.view(140, 4, 128)[~bad])
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_to_pages_of_zeros(ctx, new):
+    """Tokens of a sequence that nothing was ever written for, in pages of zeros: values of zero that all rows see alike."""
+    held = rb.KvCache(torch.zeros((40, rb.kv_page_bytes(2, 128, 4, 1024)), dtype=torch.uint8, device="cuda"), 2, 128, bits=4, page_tokens=1024)
+    tab = ints([list(range(40))])
+    k = torch.randn((20, 256), device="cuda").half()
+    ctx.kv_write(held, rb.KvBatch(ints([0, 20]), ints([20]), tab), k, k)
+    q = torch.randn((new, 8 * 128), device="cuda").half()
+    out = ctx.attend(q, held, rb.KvBatch(ints([0, new]), ints([4000]), tab))
+    want, bound = expect(held, np.arange(40)[None], [4000], [new], q, 128 ** -0.5)
+    inside(out, want, bound)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_attend_values_of_all_sizes(ctx, bits, new):
+    """Values of thousands beside values of nothing, whose scale is 2^-24 and whose weights count all the same."""
+    rng = np.random.default_rng(17)
+    lens = [33000]
+    held, table = filled(rng, 2, 128, bits, 64, lens)
+    size = torch.tensor(rng.choice([0.0, 1e-6, 1.0, 3000.0], lens[0]), device="cuda", dtype=torch.float32)[:, None]
+    k, v = (torch.randn((lens[0], 256), device="cuda") for _ in range(2))
+    batch = rb.KvBatch(ints([0, lens[0]]), ints(lens), ints(table.tolist()))
+    ctx.kv_write(held, batch, k.half(), (size * v).half())
+    q = torch.randn((new, 8 * 128), device="cuda").half()
+    for n in (lens[0], 40):
+        out = ctx.attend(q, held, rb.KvBatch(ints([0, new]), ints([n]), ints(table.tolist())))
+        want, bound = expect(held, table, [n], [new], q, 128 ** -0.5)
+        inside(out, want, bound)
+    assert ctx.last_status() == rb.ROSAQ_OK
