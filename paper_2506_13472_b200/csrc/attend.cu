@@ -12,7 +12,7 @@
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
 //
-// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 490 per pair
+// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 480 per pair
 // of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 136 us, 119 without the
 // arithmetic, 95 at the copy bandwidth.  Short calls are bound by latency: 5.7 us for one chunk, 0.9 to 1.0 us per further chunk of a warp, 5 us to join CTAs.
 // The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the device, so a captured launch

@@ -12,7 +12,7 @@
 //
 // Measured: 1.75 us per chunk and pair of tiles (head of 128), 3300 cycles: the tensor core takes 1280 of them (an MMA of 64 tokens 48 for its operands from shared memory, of 128
 // channels 64), the exponentials 1024, the terms 2560 of the shared memory's bandwidth (20 bytes per row and token: a broadcast costs as much as any load).  Softmax warps have 176
-// registers, so that terms are loaded while scores are on their way (all warps with 128: 1.78 us; a warp per tile that issues MMAs, as one for both leaves the tensor core idle).  Before the first chunk
+// registers, so that terms are loaded while scores are on their way (all warps with 128: 2 % slower).  Before the first chunk
 // and behind the last one about 8 us: the share, the queries and the first codes 4, the rows 4 (135 KB of partial sums per CTA).
 #include <algorithm>
 #include <type_traits>
