@@ -33,6 +33,8 @@ constexpr int kRows = 8;                            // query rows of a tile
 // tokens 34 and 35, 64 rows 47 and 37; of one sequence of 500 tokens 64 rows 12 and 24; of 4000 tokens 64 rows 26 and 25, 128 rows 32 and 26; of 30000 tokens 64 rows 65 and 50;
 // 128 rows behind a prefix of 500 tokens 21 and 32, of 4000 40 and 36, of 16000 76 and 46.)
 constexpr long long kManyRows = 64, kManyWork = 1ll << 22;
+// Greatest wait limit.  A warp that gives up leaves others to give up by themselves, so every wait has to end in a time that somebody can wait for; and some poll 32 times as often.
+constexpr long long kMostPolls = 1ll << 24;
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -531,7 +533,7 @@ int launch_attend(rosaq_ctx *ctx, const KvView &kv, int hd, int bits, const KvBa
   AtParams p{};
   p.kv = kv, p.b = b, p.q = q, p.out = out, p.ldq = ldq, p.ldo = ldo, p.group = n_q_heads / kv.n_heads;
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.status = ctx->d_status, p.wait_limit = ctx->wait_limit;
+  p.status = ctx->d_status, p.wait_limit = std::min<long long>(ctx->wait_limit, kMostPolls);
   const size_t prefix_bytes = prefix_tokens > 0 ? (size_t)b.n_rows * n_q_heads * (hd + 4) * sizeof(float) : 0;
   int st = ROSAQ_OK;
   if (prefix_bytes) st = grow_workspace(ctx, reinterpret_cast<void **>(&ctx->at_prefix), &ctx->at_prefix_bytes, prefix_bytes);
