@@ -422,16 +422,18 @@ int64_t rosaq_kv_page_bytes(int n_kv_heads, int head_dim, int bits, int page_tok
  *   row_start  [n_seqs + 1], must ascend: rows [row_start[i], row_start[i + 1]) of the row buffers are the new tokens of sequence i (none: nothing
  *              happens to it); rows from row_start[n_seqs] on are neither read nor written
  *   kv_len     [n_seqs] tokens of sequence i in the cache, the new ones included: they are its last ones
- *   table      [n_seqs][ld_table] pages of sequence i; token t lies in page table[i][t / page_tokens]
+ *   table      [n_seqs][ld_table] pages of sequence i; token t lies in page table[i][t / page_tokens].  Only the first table_pages entries of a row (0: all
+ *              ld_table of them) are looked at: what the rows of a wider table go on with is not this batch's
  *   prefix_table, prefix_tokens (HOST number; 0: none)   rosaq_attend: the pages of prefix_tokens further tokens that stand before every
  *              sequence; they are read once for the whole batch.  kv_len and table do not count them.
  */
 typedef struct {
   int32_t n_seqs;
-  int32_t ld_table;        /* ld_table * page_tokens <= 2^30 */
+  int32_t ld_table;        /* row stride of the table; pages of a row * page_tokens <= 2^30 */
   const int32_t *row_start, *kv_len, *table;
   const int32_t *prefix_table;
   int32_t prefix_tokens;
+  int32_t table_pages;
 } rosaq_kv_batch;
 
 /* Test hook, host only (no GPU, no context; `pages` is not read): where rosaq_kv_write, rosaq_kv_read and rosaq_attend find things for a batch whose three arrays lie

@@ -57,7 +57,7 @@ class _Kv(C.Structure):
 
 class _KvBatch(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("ld_table", C.c_int32), ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("table", C.c_void_p),
-                ("prefix_table", C.c_void_p), ("prefix_tokens", C.c_int32)]
+                ("prefix_table", C.c_void_p), ("prefix_tokens", C.c_int32), ("table_pages", C.c_int32)]
 
 
 _ARRAYS = [(C.c_void_p * n, C.c_int64 * n) for n in range(5)]   # argument arrays of rosaq_linear_multi
@@ -210,13 +210,13 @@ def kv_page_bytes(n_kv_heads, head_dim, bits, page_tokens):
     return n
 
 
-def kv_locate(row_start, kv_len, table, rows, n_pages, n_kv_heads, head_dim, bits=4, page_tokens=64):
+def kv_locate(row_start, kv_len, table, rows, n_pages, n_kv_heads, head_dim, bits=4, page_tokens=64, table_pages=0):
     """rosaq_kv_locate (host only) on lists of numbers: (status, offsets, slots) of `rows` rows."""
     ints = lambda v: (C.c_int32 * max(len(v), 1))(*v)  # noqa: E731
     n, flat = len(kv_len), ints([p for row in table for p in row])
     kv = _Kv(16, n_pages, page_tokens, n_kv_heads, head_dim, bits)
     start, lens = ints(row_start), ints(kv_len)
-    b = _KvBatch(n, len(table[0]), C.addressof(start), C.addressof(lens), C.addressof(flat), None, 0)
+    b = _KvBatch(n, len(table[0]), C.addressof(start), C.addressof(lens), C.addressof(flat), None, 0, table_pages)
     offset, slot = (C.c_int64 * max(rows, 1))(), (C.c_int32 * max(rows, 1))()
     st = lib().rosaq_kv_locate(C.byref(kv), C.byref(b), rows, offset, slot)
     return st, list(offset)[:rows], list(slot)[:rows]
@@ -236,17 +236,18 @@ class KvCache:
 
 class KvBatch:
     """rosaq_kv_batch: int32 CUDA tensors row_start [n_seqs + 1], kv_len [n_seqs], table [n_seqs][pages of a sequence] (rows contiguous), read on the
-    device whenever a call with the batch runs; prefix = (int32 CUDA tensor of its pages, number of its tokens) or None.  Keeps them alive."""
+    device whenever a call with the batch runs; prefix = (int32 CUDA tensor of its pages, number of its tokens) or None.  Keeps them alive.
+    The table may be columns of a wider one: a sequence's pages are those of `table`."""
 
     def __init__(self, row_start, kv_len, table, prefix=None):
         n = kv_len.numel()
         for t in (row_start, kv_len, table) + (() if prefix is None else (prefix[0],)):
             assert t.is_cuda and t.dtype is torch.int32 and t.stride(-1) == 1 and t.get_device() == kv_len.get_device()
         assert row_start.dim() == kv_len.dim() == 1 and row_start.numel() == n + 1 and table.dim() == 2 and table.shape[0] == n
-        assert n == 1 or table.stride(0) >= table.shape[1]
+        assert n <= 1 or table.stride(0) >= table.shape[1] > 0
         self.row_start, self.kv_len, self.table, self.prefix, self.device = row_start, kv_len, table, prefix, kv_len.get_device()
         self._s = _KvBatch(n, table.shape[1] if n == 1 else table.stride(0), row_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(),
-                           None if prefix is None else prefix[0].data_ptr(), 0 if prefix is None else int(prefix[1]))
+                           None if prefix is None else prefix[0].data_ptr(), 0 if prefix is None else int(prefix[1]), table.shape[1])
         self._p = C.addressof(self._s)
 
 

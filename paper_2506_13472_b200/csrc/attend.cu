@@ -520,7 +520,7 @@ int launch_few(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
 }
 
 int launch_any(rosaq_ctx *ctx, int hd, int bits, const AtParams &p, long long rows_of_seq, cudaStream_t s) {
-  const long long room = p.prefix_tokens > 0 ? p.prefix_tokens : (long long)p.b.ld_table * (kKvBlock << p.kv.page_shift);
+  const long long room = p.prefix_tokens > 0 ? p.prefix_tokens : (long long)p.b.width * (kKvBlock << p.kv.page_shift);
   if (rows_of_seq >= kManyRows && (double)rows_of_seq * p.b.n_seqs * p.kv.n_heads * (double)room >= (double)kManyWork) return launch_attend_rows(ctx, p, hd, bits, s);
   if (hd == 128) return bits == 4 ? launch_few<128, 4>(ctx, p, s) : launch_few<128, 8>(ctx, p, s);
   return bits == 4 ? launch_few<64, 4>(ctx, p, s) : launch_few<64, 8>(ctx, p, s);
@@ -545,7 +545,7 @@ int launch_attend(rosaq_ctx *ctx, const KvView &kv, int hd, int bits, const KvBa
     AtParams f = p;
     f.prefix_tokens = prefix_tokens, f.last_row = b.n_seqs;
     f.b.n_seqs = 1, f.b.table = prefix_table;
-    f.b.ld_table = (int)(((long long)prefix_tokens + (kKvBlock << kv.page_shift) - 1) / (kKvBlock << kv.page_shift));
+    f.b.ld_table = f.b.width = (int)(((long long)prefix_tokens + (kKvBlock << kv.page_shift) - 1) / (kKvBlock << kv.page_shift));
     st = launch_any(ctx, hd, bits, f, (long long)b.n_rows * p.group, s);
     if (st != ROSAQ_OK) return st;
   }

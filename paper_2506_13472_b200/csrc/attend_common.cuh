@@ -41,7 +41,7 @@ template <int kRows, int kTokens>
 __device__ __forceinline__ Seq load_seq(const AtParams &p, int i, bool report) {
   Seq s;
   const int first = p.b.row_start[i], end = p.b.row_start[p.prefix_tokens > 0 ? p.last_row : i + 1];
-  const int cap = p.b.ld_table * (kKvBlock << p.kv.page_shift);   // (checked on the host: at most 2^30)
+  const int cap = p.b.width * (kKvBlock << p.kv.page_shift);   // (checked on the host: at most 2^30)
   s.row = min(max(first, 0), p.b.n_rows);
   const int last = min(max(end, s.row), p.b.n_rows);
   s.rows = last - s.row;

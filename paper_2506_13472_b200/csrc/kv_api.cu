@@ -37,8 +37,10 @@ int check_batch(const rosaq_kv_batch *b, const rosaq_kv *kv, int n_rows, KvBatch
   if (!b || b->n_seqs < 1 || b->ld_table < 1 || !b->row_start || !b->kv_len || !b->table) return ROSAQ_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(b->row_start) | reinterpret_cast<uintptr_t>(b->kv_len) | reinterpret_cast<uintptr_t>(b->table)) & 3)
     return ROSAQ_ERR_ALIGNMENT;
-  if ((int64_t)b->ld_table * kv->page_tokens > (int64_t)1 << 30) return ROSAQ_ERR_UNSUPPORTED_SHAPE;
-  *out = KvBatchView{b->row_start, b->kv_len, b->table, b->n_seqs, b->ld_table, n_rows};
+  if (b->table_pages < 0 || b->table_pages > b->ld_table) return ROSAQ_ERR_INVALID_ARG;
+  const int width = b->table_pages > 0 ? b->table_pages : b->ld_table;
+  if ((int64_t)width * kv->page_tokens > (int64_t)1 << 30) return ROSAQ_ERR_UNSUPPORTED_SHAPE;
+  *out = KvBatchView{b->row_start, b->kv_len, b->table, b->n_seqs, b->ld_table, width, n_rows};
   return ROSAQ_OK;
 }
 

@@ -41,6 +41,7 @@ struct KvView {
 struct KvBatchView {
   const int32_t *row_start, *kv_len, *table;
   int n_seqs, ld_table;
+  int width;            // entries of a row of the table that belong to it
   int n_rows;           // rows of the caller's buffers
 };
 
@@ -70,7 +71,7 @@ __host__ __device__ inline KvPlace kv_place(const KvView &kv, const KvBatchView 
   const long long len = b.kv_len[seq];
   p->row = row, p->n = end - row, p->slot = 0, p->offset = -1;
   if (end <= row) return kBadRows;                    // (not ascending)
-  if (begin < 0 || begin > row || len < (long long)stop - begin || len > ((long long)b.ld_table << kv.page_shift) * kKvBlock) return kBadSequence;
+  if (begin < 0 || begin > row || len < (long long)stop - begin || len > ((long long)b.width << kv.page_shift) * kKvBlock) return kBadSequence;
   const long long pos = len - (stop - row);
   p->slot = (int)(pos % kKvBlock);
   if (p->n > kKvBlock - p->slot) p->n = kKvBlock - p->slot;

@@ -35,3 +35,29 @@ def test_long_wait_limits(ctx, new):
     status = ctx.last_status()
     ctx.set_wait_limit(limit)
     assert status == rb.ROSAQ_OK and same(got, want)
+
+
+@pytest.mark.parametrize("new", [1, 48])                                    # the second one: many rows
+def test_columns_of_a_wider_table(ctx, new):
+    """The pages of a sequence are those of the table, not what its rows go on with in memory: lengths past them are cut and reported."""
+    rng = np.random.default_rng(25)
+    lens = [2048, 1024, 2048]
+    held, table = filled(rng, 4, 128, 4, 1024, [4096] * 3)
+    fill(ctx, rng, held, table, [4096] * 3)
+    q = torch.randn((3 * new, 16 * 128), device="cuda").half()
+    wide = ints(table.tolist())
+    assert wide.shape[1] == 4
+    want = ctx.attend(q, held, rb.KvBatch(starts([new] * 3), ints(lens), wide[:, :2].contiguous())).clone()
+    assert same(ctx.attend(q, held, rb.KvBatch(starts([new] * 3), ints(lens), wide[:, :2])), want) and ctx.last_status() == rb.ROSAQ_OK
+    want = ctx.attend(q, held, rb.KvBatch(starts([new] * 3), ints([2048] * 3), wide[:, :2])).clone()
+    kept = held.pages.clone()
+    long = rb.KvBatch(starts([new] * 3), ints([2048, 2049, 2048]), wide[:, :2])
+    got = ctx.attend(q, held, long)
+    assert ctx.last_status() == rb.ROSAQ_ERR_INVALID_ARG
+    for i in (0, 2):
+        assert same(got[i * new:i * new + new], want[i * new:i * new + new])
+    x = torch.randn((3 * new, 4 * 128), device="cuda").half()
+    ctx.kv_write(held, long, x, x)
+    assert ctx.last_status() == rb.ROSAQ_ERR_INVALID_ARG and torch.equal(held.pages[table[1]], kept[table[1]])
+    ctx.kv_read(held, long, 3 * new)
+    assert ctx.last_status() == rb.ROSAQ_ERR_INVALID_ARG

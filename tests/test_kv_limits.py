@@ -1,0 +1,24 @@
+"""Limits of the quantized cache's batches that the host sees: no GPU needed."""
+import pytest
+
+from paper_2506_13472_b200 import binding as rb
+from tests.test_kv_arguments import INVALID, ROWS, SHAPE, batch, kv, rows_call
+
+
+@pytest.mark.parametrize("name", ["rosaq_kv_write", "rosaq_kv_read", "rosaq_attend"])
+def test_columns_of_a_table_refused(name):
+    for change, want in ((dict(table_pages=-1), INVALID), (dict(table_pages=4), INVALID), (dict(ld_table=1 << 25, table_pages=(1 << 24) + 1), SHAPE)):
+        assert rows_call(name, kv(), batch(**change), ROWS, 256, 2 * ROWS, 256, 5) == want, change
+    for change in (dict(table_pages=3), dict(table_pages=1), dict(ld_table=1 << 25, table_pages=1 << 24)):
+        assert rows_call(name, kv(), batch(**change), ROWS, 256, 2 * ROWS, 256, 0) == rb.ROSAQ_OK, change
+
+
+def test_locate_in_columns_of_a_wider_table():
+    """The first pages of each row belong to the batch: lengths past them do not fit, whatever stands there."""
+    size = rb.kv_page_bytes(2, 64, 4, 32)
+    table = [[1, 2, 3, 4], [5, 6, 0, 1]]
+    where = lambda lens, pages: rb.kv_locate([0, 1, 2], lens, table, 2, 7, 2, 64, 4, 32, table_pages=pages)  # noqa: E731
+    assert where([97, 33], 0) == (rb.ROSAQ_OK, [4 * size, 6 * size], [0, 0])
+    assert where([64, 33], 2) == (rb.ROSAQ_OK, [2 * size + 4 * 64 * 4 + 128, 6 * size], [15, 0])
+    assert where([65, 33], 2) == (INVALID, [-1, 6 * size], [-1, 0])
+    assert where([1, 128], 2) == (INVALID, [size, -1], [0, -1])
