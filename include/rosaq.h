@@ -431,7 +431,7 @@ typedef struct {
   int32_t n_seqs;
   int32_t ld_table;        /* row stride of the table; pages of a row * page_tokens <= 2^30 */
   const int32_t *row_start, *kv_len, *table;
-  const int32_t *prefix_table;
+  const int32_t *prefix_table;   /* prefix_tokens / page_tokens entries, rounded up */
   int32_t prefix_tokens;
   int32_t table_pages;
 } rosaq_kv_batch;

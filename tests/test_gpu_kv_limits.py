@@ -61,3 +61,23 @@ def test_columns_of_a_wider_table(ctx, new):
     assert ctx.last_status() == rb.ROSAQ_ERR_INVALID_ARG and torch.equal(held.pages[table[1]], kept[table[1]])
     ctx.kv_read(held, long, 3 * new)
     assert ctx.last_status() == rb.ROSAQ_ERR_INVALID_ARG
+
+
+def test_short_page_lists_of_a_prefix_refused(ctx):
+    """A list of fewer pages than the prefix has tokens for is refused before anything is launched; one of exactly as many is not."""
+    rng = np.random.default_rng(26)
+    held, table = filled(rng, 2, 64, 4, 16, [100, 40])
+    fill(ctx, rng, held, table, [100, 40])
+    q = torch.randn((1, 2 * 64), device="cuda").half()
+    call = lambda pages, n: ctx.attend(q, held, rb.KvBatch(ints([0, 1]), ints([40]), ints(table[1:].tolist()), prefix=(pages, n)))  # noqa: E731
+    pages = ints(table[0].tolist())
+    assert pages.shape[0] == 7
+    want = call(pages, 96).clone()
+    assert same(call(pages[:6], 96), want) and ctx.last_status() == rb.ROSAQ_OK
+    for short, n in ((pages[:6], 97), (pages[:1], 100), (pages[:0], 1)):
+        with pytest.raises(AssertionError):
+            call(short, n)
+    with pytest.raises(AssertionError):
+        call(pages.view(1, 7), 96)
+    call(pages[:0], 0)
+    assert ctx.last_status() == rb.ROSAQ_OK
