@@ -198,17 +198,18 @@ __device__ __forceinline__ void read_block(const KvPiece &p, __half *x, long lon
   const int lane = threadIdx.x & 31, part = lane % kLanes, mine = lane / kLanes;
   const uint8_t *const params = block + 2 * kv_code_bytes(kHd, kBits) + (kValue ? 4 * kKvBlock : 0);
   const uint8_t *const codes = block + (kValue ? kv_code_bytes(kHd, kBits) : 0) + 16 * lane;
+  // (plain loads: the launch before may have been writing these bytes after this one had begun, which loads by way of the read-only path do not allow)
   uint4 in[kWords / 4];
 #pragma unroll
-  for (int q = 0; q < kWords / 4; ++q) in[q] = __ldg(reinterpret_cast<const uint4 *>(codes + 512 * q));
+  for (int q = 0; q < kWords / 4; ++q) in[q] = *reinterpret_cast<const uint4 *>(codes + 512 * q);
   // scale and least value of the four (two: keys) tokens whose codes this lane holds
   uint32_t prm[4];
   if (kValue) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2 *>(params + 8 * (lane & 3))), v = __ldg(reinterpret_cast<const uint2 *>(params + 32 + 8 * (lane & 3)));
+    const uint2 u = *reinterpret_cast<const uint2 *>(params + 8 * (lane & 3)), v = *reinterpret_cast<const uint2 *>(params + 32 + 8 * (lane & 3));
     prm[0] = u.x, prm[1] = u.y, prm[2] = v.x, prm[3] = v.y;
   } else {
-    prm[0] = prm[1] = __ldg(reinterpret_cast<const uint32_t *>(params + 4 * (lane >> 2)));
-    prm[2] = prm[3] = __ldg(reinterpret_cast<const uint32_t *>(params + 32 + 4 * (lane >> 2)));
+    prm[0] = prm[1] = *reinterpret_cast<const uint32_t *>(params + 4 * (lane >> 2));
+    prm[2] = prm[3] = *reinterpret_cast<const uint32_t *>(params + 32 + 4 * (lane >> 2));
   }
   float s[4], lo[4];
 #pragma unroll

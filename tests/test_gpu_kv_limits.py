@@ -81,3 +81,31 @@ def test_short_page_lists_of_a_prefix_refused(ctx):
         call(pages.view(1, 7), 96)
     call(pages[:0], 0)
     assert ctx.last_status() == rb.ROSAQ_OK
+
+
+def test_reads_between_writes(ctx):
+    """Writes and reads of the same tokens in turn, captured, none waiting for the host: each read returns what was written last."""
+    rng = np.random.default_rng(27)
+    lens, turns = [700, 90], 8
+    held, table = filled(rng, 8, 128, 8, 64, lens)
+    batch = rb.KvBatch(starts(lens), ints(lens), ints(table.tolist()))
+    xs = [torch.randn((790, 8 * 128), device="cuda").half() for _ in range(turns)]
+    want = []
+    for x in xs:
+        ctx.kv_write(held, batch, x, -x)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in ctx.kv_read(held, batch, 790)])
+        torch.cuda.synchronize()
+    outs = [[torch.empty_like(x) for _ in range(2)] for x in xs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x, (k, v) in zip(xs, outs):
+            ctx.kv_read(held, batch, 790, k=k, v=v)
+            ctx.kv_write(held, batch, x, -x)
+            ctx.kv_read(held, batch, 790, k=k, v=v)
+    for _ in range(20):
+        graph.replay()
+    torch.cuda.synchronize()
+    for (k, v), (kw, vw) in zip(outs, want):
+        assert same(k, kw) and same(v, vw)
+    assert ctx.last_status() == rb.ROSAQ_OK
