@@ -215,10 +215,12 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) most_q = fmaxf(most_q, __shfl_xor_sync(0xffffffffu, most_q, d));
     sum += __shfl_xor_sync(0xffffffffu, sum, 1), sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    // (Infinities among the queries make all scores NaN: over keys of one sign they would all be minus infinity, and the row like one that sees nothing.)
+    const float row_sum = isfinite(sum) ? p.scale_log2 * sum : NAN;
     const int seen = p.prefix_tokens > 0 || !valid ? s.len : min(max(seen0 + tok, 0), s.len);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      row_b[e] = __shfl_sync(0xffffffffu, p.scale_log2 * sum, 4 * (2 * c + e));
+      row_b[e] = __shfl_sync(0xffffffffu, row_sum, 4 * (2 * c + e));
       lim[e] = __shfl_sync(0xffffffffu, seen, 4 * (2 * c + e));
     }
     const int up = most_q > 0.f ? 12 - ((int)(__float_as_uint(most_q) >> 23) - 127) : 0;   // (fp16 values: never an fp32 subnormal)

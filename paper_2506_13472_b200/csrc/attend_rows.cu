@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
 #pragma unroll
           for (int k = 0; k < 4; ++k) sum_q += __low2float(h[k]) + __high2float(h[k]);
         }
+        if (!isfinite(sum_q)) sum_q = NAN;           // all scores are NaN then: over keys of one sign they could all be minus infinity, and the row like one that sees nothing
         const int lim = p.prefix_tokens > 0 ? s.len : valid ? min(max(s.len - s.rows + 1 + tok, 0), s.len) : s.len;
         const int least = __reduce_min_sync(0xffffffffu, lim);
         for (int j = 0; j < sg.count; ++j, ++g) {

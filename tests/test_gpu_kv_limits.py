@@ -109,3 +109,25 @@ def test_reads_between_writes(ctx):
     for (k, v), (kw, vw) in zip(outs, want):
         assert same(k, kw) and same(v, vw)
     assert ctx.last_status() == rb.ROSAQ_OK
+
+
+@pytest.mark.parametrize("new,prefix", [(1, 0), (1, 2000), (40, 0)])     # the last one: many rows
+@pytest.mark.parametrize("bits,sign", [(4, 1.0), (4, -1.0), (8, 1.0)])
+def test_infinite_queries_over_keys_of_one_sign(ctx, new, prefix, bits, sign):
+    """Every score of such a row is minus infinity: NaN, and not the zeros of a row that sees nothing."""
+    rng = np.random.default_rng(21)
+    lens = [prefix or 16, 8200, 90]
+    held, table = filled(rng, 4, 128, bits, 64, lens)
+    k, v = (torch.randn((sum(lens), 512), device="cuda") for _ in range(2))
+    k = 10 + k.clamp(-4, 4)
+    k[:, 5::128] = 30.0                                       # the greatest of every head, whose codes are the greatest too
+    ctx.kv_write(held, rb.KvBatch(starts(lens), ints(lens), ints(table.tolist())), k.half(), v.half())
+    q = torch.randn((2 * new, 4 * 4 * 128), device="cuda").half()
+    batch = rb.KvBatch(starts([new, new]), ints(lens[1:]), ints(table[1:].tolist()), prefix=(ints(table[0].tolist()), prefix) if prefix else None)
+    clean = ctx.attend(q, held, batch, scale=sign * 0.1)
+    q[new - 1, 5], q[2 * new - 1, 7 * 128 + 5] = -sign * float("inf"), -sign * float("inf")
+    got = ctx.attend(q, held, batch, scale=sign * 0.1).view(2 * new, 16, 128)
+    bad = torch.zeros((2 * new, 16), dtype=torch.bool, device="cuda")
+    bad[new - 1, 0] = bad[2 * new - 1, 7] = True
+    assert torch.isnan(got[bad]).all() and not torch.isnan(got[~bad]).any()
+    assert same(got[~bad], clean.view(2 * new, 16, 128)[~bad])
