@@ -70,7 +70,7 @@ struct Cfg {
   static constexpr int kPerSm = 2;
   static constexpr int kAccLd = kHd + 4;            // floats: two rows of a pair on different banks
   static constexpr int kPartBytes = kRows * (4 * kAccLd + 16);   // a part of a tile: [row][kAccLd], then [row]{maximum, sum, sum of least values, -}
-  static constexpr int kPairBytes = kTokens * 20;   // of a warp: what its tokens' pairs become
+  static constexpr int kPairBytes = kTokens * 20 + kRows * 4;   // of a warp: what its tokens' pairs become, and what brings the scores of rows back that were scaled by themselves
   static constexpr int kFixed = kPairBytes + 2 * (int)sizeof(OpenTile) + 16;   // of a warp, besides its slots
   static constexpr int kRoom = 222 * 1024 / kPerSm - 1024 - 128 - (kFixed + 64) * kWarps;
   static constexpr int kDepth = kRoom / kStageBytes / kWarps < 32 / kWarps ? kRoom / kStageBytes / kWarps : 32 / kWarps;   // slots of a warp, next to each other
@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
   constexpr int kBlockBytes = kv_block_bytes(kHd, kBits);
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t *const ring = smem;                                                             // [warp][kDepth] slots
-  float4 *const pair_terms = reinterpret_cast<float4 *>(smem + C::kStages * C::kStageBytes);   // [warp][token]{s_k', lo_k, log2 s_v, 1 / s_v}, [token] lo_v / s_v + middle
+  float4 *const pair_terms = reinterpret_cast<float4 *>(smem + C::kStages * C::kStageBytes);   // [warp][token]{s_k', lo_k, log2 s_v, 1 / s_v}, [token] lo_v / s_v + middle, [row]
   uint64_t *const bars = reinterpret_cast<uint64_t *>(pair_terms + C::kPairBytes / 16 * kWarps);
   const float **const data = reinterpret_cast<const float **>(bars + 2 * C::kStages);     // [warp][2]: where the parts below lie
   OpenTile *const parts = reinterpret_cast<OpenTile *>(data + 2 * kWarps);                // [warp]{first part of a tile that began before, last one}
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
   // ---- consumers
   const int r = lane >> 2, c = lane & 3;
   float4 *const terms = pair_terms + warp * (C::kPairBytes / 16);
-  float *const term_vl = reinterpret_cast<float *>(terms + kTokens);
+  float *const term_vl = reinterpret_cast<float *>(terms + kTokens), *const back = term_vl + kTokens;
   bool lost = false;
   int j = bound(warp);                               // this warp's next chunk
   const int last = bound(warp + 1);
@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
     const int first_row = tile * kRows, n_flat = s.rows * p.group;
 
     // ---- query rows of the tile: B fragments, scaled by a power of two so that the greatest value of all rows lies in [2^12, 2^13); of the channels whose
-    // nibbles read sixteen times too large a sixteenth.  Rows that are not finite do not count for it.
+    // nibbles read sixteen times too large a sixteenth.  Rows that are not finite do not count for it.  fp16 holds what is left of a row exactly down to 2^-16 of its greatest value, and
+    // what lies below to 2^-27 of it, as long as that is no more than 2^kQuiet below the tile's; where one is, every row is scaled by itself, and its scores are brought back by a product.
     uint32_t qf[kSteps][2];
     float row_b[2];                                  // scale log2(e) sum(q) of this lane's columns 2 c, 2 c + 1
     int lim[2];                                      // tokens that the row sees
@@ -212,8 +213,10 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
         sum += x.x + x.y;
       }
     if (!(most_q <= 65504.f)) most_q = 0.f;
+    most_q = fmaxf(most_q, __shfl_xor_sync(0xffffffffu, most_q, 1)), most_q = fmaxf(most_q, __shfl_xor_sync(0xffffffffu, most_q, 2));
+    const float own_q = most_q;                      // of this lane's row
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) most_q = fmaxf(most_q, __shfl_xor_sync(0xffffffffu, most_q, d));
+    for (int d = 16; d > 2; d /= 2) most_q = fmaxf(most_q, __shfl_xor_sync(0xffffffffu, most_q, d));
     sum += __shfl_xor_sync(0xffffffffu, sum, 1), sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     // (Infinities among the queries make all scores NaN: over keys of one sign they would all be minus infinity, and the row like one that sees nothing.)
     const float row_sum = isfinite(sum) ? p.scale_log2 * sum : NAN;
@@ -225,11 +228,17 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
     }
     const int up = most_q > 0.f ? 12 - ((int)(__float_as_uint(most_q) >> 23) - 127) : 0;   // (fp16 values: never an fp32 subnormal)
     const float key_scale = p.scale_log2 * __uint_as_float((uint32_t)(127 + 24 - up) << 23);
+    constexpr int kQuiet = 6;
+    const int own_up = own_q > 0.f ? 12 - ((int)(__float_as_uint(own_q) >> 23) - 127) : up;
+    const bool apart = __any_sync(0xffffffffu, own_up > up + kQuiet);
+    const int row_up = apart ? own_up : up;
+    if (apart && c == 0) back[r] = __uint_as_float((uint32_t)(127 + up - own_up) << 23);
+    __syncwarp();
 #pragma unroll
     for (int k = 0; k < kSteps; ++k)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float f = __uint_as_float((uint32_t)(127 + up - (kBits == 4 && h ? 4 : 0)) << 23);
+        const float f = __uint_as_float((uint32_t)(127 + row_up - (kBits == 4 && h ? 4 : 0)) << 23);
         const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&qf[k][h]));
         qf[k][h] = pack_h2(x.x * f, x.y * f);
       }
@@ -314,6 +323,13 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
               code_fragment<kBits, false>(w[b], e, a);
               mma16816(sc[b], a, qf[kPer * i + e][0], qf[kPer * i + e][1]);
             }
+        }
+        if (apart) {
+          const float2 f = *reinterpret_cast<const float2 *>(back + 2 * c);
+#pragma unroll
+          for (int b = 0; b < kChunk; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sc[b][2 * h] *= f.x, sc[b][2 * h + 1] *= f.y;
         }
         // ---- u = score log2(e) + log2(s_v)
         float vi[kChunk][2], vl[kChunk][2];

@@ -132,6 +132,32 @@ def attention(q, kv, seen, scale):
     return torch.where(any_seen, out, torch.zeros_like(out)), bound
 
 
+def attention_norm(q, kv, seen, scale, updates=128):
+    """(out, bound) as attention(), with a bound [n][hq] of the norm of a row and head's error.
+
+    In terms of w = p / sum p and S = sqrt(sum w^2 |v - out|^2), the norm that errors of the weights add up to when they are independent:
+      2^-11 |out|                    the result's rounding
+      2 * 2^-11 S                    the weights' 11 bits, the same in products and sums.  Each is off by at most 2^-11 and by 0.42 * 2^-11 in the mean square (an
+                                     error uniform in half a step either way, a mantissa of logarithmic density): nearly five deviations, and for up to four tokens the worst case
+      updates 2^-23 * 4 (|out| + S)  accumulators: each update cuts off less than 2^-23 of what they hold, a walk of no more than some S
+      2^-20 (1 + m) sum w |v - out|  scores, as in attention()
+    and half a step of a subnormal result per channel."""
+    (kc, kl, _), (vc, vl, _) = kv
+    n, hq, hd = q.shape
+    rep = lambda x: x.repeat_interleave(hq // kc.shape[1], 1)  # noqa: E731
+    hide = ~seen[:, None, :]
+    scores = (torch.einsum("nhd,thd->nht", q, rep(kc + kl)) * scale).masked_fill(hide, -math.inf)
+    m = (torch.einsum("nhd,thd->nht", q.abs(), rep(kc)) + q.sum(-1, keepdim=True).abs() * rep(kl)[..., 0].T.abs()[None]) * abs(scale)
+    m = m.masked_fill(hide, 0).amax(-1)
+    w, v = torch.softmax(scores, -1).nan_to_num(0.0), rep(vc + vl)
+    out = torch.einsum("nht,thd->nhd", w, v)
+    size = out.norm(dim=-1)
+    away = (v.pow(2).sum(-1).T[None] - 2 * torch.einsum("nhd,thd->nht", out, v) + size[..., None] ** 2).clamp(min=0)
+    s = (w ** 2 * away).sum(-1).sqrt()
+    bound = 2.0 ** -11 * (size + 2 * s) + updates * 2.0 ** -21 * (size + s) + 2.0 ** -20 * (1 + m) * (w * away.sqrt()).sum(-1) + 2.0 ** -25 * hd ** 0.5
+    return out, bound
+
+
 def rope(x, positions, freq, rot, interleaved, magnitude):
     """(y, bound) of fp16 heads x [rows][heads][hd], 64 bits; freq [rot / 2]."""
     x = np.asarray(x, np.float16).astype(np.float64)

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2506_13472_b200 import binding as rb
+from tests import kv_reference as ref
 from tests.test_gpu_kv_attention import fill, filled, ints, same
 
 pytestmark = pytest.mark.gpu
@@ -131,3 +132,31 @@ def test_infinite_queries_over_keys_of_one_sign(ctx, new, prefix, bits, sign):
     bad[new - 1, 0] = bad[2 * new - 1, 7] = True
     assert torch.isnan(got[bad]).all() and not torch.isnan(got[~bad]).any()
     assert same(got[~bad], clean.view(2 * new, 16, 128)[~bad])
+
+
+@pytest.mark.parametrize("quiet,loud,key", [(2.0 ** -11, 60000.0, 60000.0), (2.0 ** -7, 30000.0, 4000.0), (0.1, 100.0, 300.0), (2.0 ** -20, 1.0, 60000.0)])
+@pytest.mark.parametrize("bits,prefix", [(4, 0), (8, 0), (4, 900)])
+def test_queries_of_very_different_sizes(ctx, bits, prefix, quiet, loud, key):
+    """A row's result does not depend on how large the rows beside it are."""
+    rng = np.random.default_rng(22)
+    lens = [prefix or 16, 600, 31, 300]
+    held, table = filled(rng, 2, 128, bits, 64, lens)
+    k, v = (torch.randn((sum(lens), 256), device="cuda") for _ in range(2))
+    ctx.kv_write(held, rb.KvBatch(starts(lens), ints(lens), ints(table.tolist())), (key * k / 4.5).half(), v.half())
+    q = torch.randn((3, 8, 128), device="cuda").clamp(-4, 4) / 4
+    size = torch.full((3, 8, 1), quiet, device="cuda")
+    size[0, 1] = size[0, 6] = size[2, 4] = loud
+    size[1, 3] = 0.0
+    q = (q * size).half().view(3, -1)
+    pre = (ints(table[0].tolist()), prefix) if prefix else None
+    out = ctx.attend(q, held, rb.KvBatch(starts([1, 1, 1]), ints(lens[1:]), ints(table[1:].tolist()), prefix=pre))
+    few = (size < loud).view(3, 8)
+    args = (held.pages, 2, 128, bits, 64)
+    for i in range(3):
+        kv = ref.values(*args, ints(table[i + 1].tolist()), lens[i + 1])
+        if pre:
+            kv = [[torch.cat([a, b]) for a, b in zip(x, y)] for x, y in zip(ref.values(*args, *pre), kv)]
+        seen = torch.ones((1, kv[0][0].shape[0]), dtype=torch.bool, device="cuda")
+        want, bound = ref.attention_norm(q[i:i + 1].double().view(1, 8, 128), kv, seen, 128 ** -0.5)
+        off = (out[i:i + 1].double().view(1, 8, 128) - want).norm(dim=-1)
+        assert bool((off <= bound)[0, few[i]].all()), (off / bound)[0, few[i]].max()
