@@ -456,7 +456,7 @@ int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batc
  * g = n_q_heads / n_kv_heads (a whole number).  The row of new token j of sequence i sees the prefix and the first
  * kv_len[i] - (row_start[i + 1] - row_start[i]) + j + 1 tokens of its sequence; a row that sees nothing becomes zeros.
  * Products of fp16 q and codes are exact (but for elements of q below 2^-16 of their row's greatest, which may be off by 2^-27 of that) and summed in fp32; softmax weights have the 11 bits of an fp16 number, in the product with the value codes and in their
- * fp32 sums; out is rounded once.  Calls of many rows (64 and more query rows per sequence and key/value head, and enough room in the table) run on another kernel of the
+ * fp32 sums; out is rounded once, to 65504 at most.  Calls of many rows (64 and more query rows per sequence and key/value head, and enough room in the table) run on another kernel of the
  * same arithmetic, so their bits may differ from those of fewer rows.  Rows of q that hold infinities or NaNs make their own results NaN and no others.
  * The cache is cut into equal shares over the SMs on the device, from kv_len.  Repeated calls give the same bits; other kv_len of other sequences change
  * the order of the fp32 sums only.  out may be q (same stride); any other overlap is ROSAQ_ERR_INVALID_ARG.

@@ -448,13 +448,16 @@ __global__ void __launch_bounds__(32 * (kWarps + 1), Cfg<kHd, kBits, kWarps>::kP
           const float inv = l == 0.f ? 0.f : 1.f / l;   // no token: zeros
           f *= inv, g *= inv;
 #pragma unroll
-          for (int k = 0; k < kSteps; ++k)
+          for (int k = 0; k < kSteps; ++k) {
+            float x[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float x = (acc[k][e + 2 * h] + off[e]) * f;
-              if (to.prefix) x = __fmaf_rn(pre[k][h], g, x);
-              to.out[16 * k + 8 * h + r] = __float2half_rn(x);
+              x[h] = (acc[k][e + 2 * h] + off[e]) * f;
+              if (to.prefix) x[h] = __fmaf_rn(pre[k][h], g, x[h]);
             }
+            const uint32_t both = pack_out(x[0], x[1]);
+            to.out[16 * k + r] = __ushort_as_half((unsigned short)both), to.out[16 * k + 8 + r] = __ushort_as_half((unsigned short)(both >> 16));
+          }
         }
       }
     }

@@ -77,6 +77,11 @@ __device__ __forceinline__ uint32_t pack_h2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t *>(&h);
 }
+// Two results: fp16, 65504 at most, as rosaq_kv_read has it.  (The greatest code of a head that reaches to the end of fp16 stands for up to 65566.)  A NaN stays one.
+__device__ __forceinline__ uint32_t pack_out(float a, float b) {
+  const __half2 h = __hmin2_nan(__floats2half2_rn(a, b), __half2half2(__ushort_as_half(0x7bff)));
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
 
 __device__ __forceinline__ uint32_t h2_fma(uint32_t v, uint32_t mul, uint32_t add) {
   const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&mul), *reinterpret_cast<const __half2 *>(&add));
@@ -228,7 +233,7 @@ __device__ __forceinline__ void store_row4(const AtParams &p, const RowAt &at, i
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;        // no token: zeros
   uint2 h;
-  h.x = pack_h2(a.x * inv, a.y * inv), h.y = pack_h2(a.z * inv, a.w * inv);
+  h.x = pack_out(a.x * inv, a.y * inv), h.y = pack_out(a.z * inv, a.w * inv);
   *reinterpret_cast<uint2 *>(at.out + ch) = h;
 }
 

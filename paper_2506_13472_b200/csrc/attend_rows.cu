@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_rows_kernel(const __grid_c
                 v = make_float4(__fmaf_rn(w.x, gg, v.x), __fmaf_rn(w.y, gg, v.y), __fmaf_rn(w.z, gg, v.z), __fmaf_rn(w.w, gg, v.w));
               }
               uint2 h;
-              h.x = pack_h2(v.x, v.y), h.y = pack_h2(v.z, v.w);
+              h.x = pack_out(v.x, v.y), h.y = pack_out(v.z, v.w);
               *reinterpret_cast<uint2 *>(to_out + at) = h;
             } else {
               *reinterpret_cast<float4 *>(to_sums + at) = v;

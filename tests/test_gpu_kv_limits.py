@@ -5,7 +5,7 @@ import torch
 
 from paper_2506_13472_b200 import binding as rb
 from tests import kv_reference as ref
-from tests.test_gpu_kv_attention import fill, filled, ints, same
+from tests.test_gpu_kv_attention import expect, fill, filled, inside, ints, same
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,22 @@ def test_queries_of_very_different_sizes(ctx, bits, prefix, quiet, loud, key):
         want, bound = ref.attention_norm(q[i:i + 1].double().view(1, 8, 128), kv, seen, 128 ** -0.5)
         off = (out[i:i + 1].double().view(1, 8, 128) - want).norm(dim=-1)
         assert bool((off <= bound)[0, few[i]].all()), (off / bound)[0, few[i]].max()
+
+
+@pytest.mark.parametrize("new,prefix", [(1, 0), (1, 500), (40, 0)])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_results_at_the_end_of_fp16(ctx, bits, new, prefix):
+    """Heads from -65504 to 65504: what a code stands for may lie past 65504, a result does not."""
+    rng = np.random.default_rng(23)
+    lens = [prefix or 16, 8200]
+    held, table = filled(rng, 4, 128, bits, 64, lens)
+    k, v = (torch.randn((sum(lens), 512), device="cuda").half() for _ in range(2))
+    v[:, 3::128], v[:, 4::128] = 65504.0, -65504.0
+    ctx.kv_write(held, rb.KvBatch(starts(lens), ints(lens), ints(table.tolist())), k, v)
+    q = torch.randn((new, 16 * 128), device="cuda").half()
+    pre = (ints(table[0].tolist()), prefix) if prefix else None
+    out = ctx.attend(q, held, rb.KvBatch(starts([new]), ints(lens[1:]), ints(table[1:].tolist()), prefix=pre))
+    want, bound = expect(held, table[1:], lens[1:], [new], q, 128 ** -0.5, pre)
+    assert bool((want > 65520).any())
+    inside(out, want.clamp(max=65504), bound)
+    assert torch.all(out.view(new, 16, 128)[..., 3] == 65504)
