@@ -454,7 +454,7 @@ int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batc
 /*
  * out[n_rows][ldo] = softmax(scale q k^T) v per row and query head over the values held in the cache; query heads [j g, (j + 1) g) share key/value head j,
  * g = n_q_heads / n_kv_heads (a whole number).  The row of new token j of sequence i sees the prefix and the first
- * kv_len[i] - (row_start[i + 1] - row_start[i]) + j + 1 tokens of its sequence; a row that sees nothing becomes zeros.
+ * kv_len[i] - (row_start[i + 1] - row_start[i]) + j + 1 tokens of its sequence; a row that sees nothing becomes zeros.  |scale| <= 2^58.
  * Products of fp16 q and codes are exact (but for elements of q below 2^-16 of their row's greatest, which may be off by 2^-27 of that) and summed in fp32; softmax weights have the 11 bits of an fp16 number, in the product with the value codes and in their
  * fp32 sums; out is rounded once, to 65504 at most.  Calls of many rows (64 and more query rows per sequence and key/value head, and enough room in the table) run on another kernel of the
  * same arithmetic, so their bits may differ from those of fewer rows.  Rows of q that hold infinities or NaNs make their own results NaN and no others.

@@ -183,7 +183,9 @@ int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batc
 
 int rosaq_attend(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, const void *q, int64_t ldq, int n_q_heads, float scale,
                  void *out, int64_t ldo, int n_rows, void *stream) {
-  if (!ctx || n_q_heads < 1 || !std::isfinite(scale)) return ROSAQ_ERR_INVALID_ARG;
+  if (!ctx || n_q_heads < 1) return ROSAQ_ERR_INVALID_ARG;
+  // scores of fp16 numbers stay below 2^99.2 then, above what the kernels take for a row that has seen nothing (-10^30)
+  if (!(std::fabs(scale) <= 288230376151711744.f)) return ROSAQ_ERR_INVALID_ARG;
   KvView view;
   KvBatchView b;
   int st = check_kv(kv, &view);

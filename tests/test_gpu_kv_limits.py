@@ -179,3 +179,23 @@ def test_results_at_the_end_of_fp16(ctx, bits, new, prefix):
     assert bool((want > 65520).any())
     inside(out, want.clamp(max=65504), bound)
     assert torch.all(out.view(new, 16, 128)[..., 3] == 65504)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("scale", [2.0 ** 58, 1e12])
+def test_scores_far_below_zero(ctx, new, scale):
+    """The greatest scale over the greatest queries and keys, every score negative: the token of the least of them has the whole weight."""
+    rng = np.random.default_rng(28)
+    lens = [8200]
+    held, table = filled(rng, 4, 128, 4, 64, lens)
+    k = torch.full((8200, 512), -65504.0, device="cuda").half()
+    k[7] = -60000.0
+    v = torch.randn((8200, 512), device="cuda").half()
+    batch = rb.KvBatch(starts(lens), ints(lens), ints(table.tolist()))
+    ctx.kv_write(held, batch, k, v)
+    v = ctx.kv_read(held, batch, 8200)[1]
+    q = torch.full((new, 16 * 128), 65504.0, device="cuda").half()
+    out = ctx.attend(q, held, rb.KvBatch(starts([new]), ints(lens), ints(table.tolist())), scale=scale)
+    want = v[7].double().view(4, 1, 128).expand(4, 4, 128).reshape(1, -1).expand(new, -1)
+    # (a read is rounded to fp16 too: half a step each, and what a scale's logarithm and reciprocal are off by)
+    inside(out, want, 2 * 2.0 ** -11 * want.abs() + 2.0 ** -19 * 16)

@@ -1,8 +1,10 @@
 """Limits of the quantized cache's batches that the host sees: no GPU needed."""
+import ctypes as C
+
 import pytest
 
 from paper_2506_13472_b200 import binding as rb
-from tests.test_kv_arguments import INVALID, ROWS, SHAPE, batch, kv, rows_call
+from tests.test_kv_arguments import CTX, INVALID, ROWS, SHAPE, batch, kv, rows_call
 
 
 @pytest.mark.parametrize("name", ["rosaq_kv_write", "rosaq_kv_read", "rosaq_attend"])
@@ -22,3 +24,11 @@ def test_locate_in_columns_of_a_wider_table():
     assert where([64, 33], 2) == (rb.ROSAQ_OK, [2 * size + 4 * 64 * 4 + 128, 6 * size], [15, 0])
     assert where([65, 33], 2) == (INVALID, [-1, 6 * size], [-1, 0])
     assert where([1, 128], 2) == (INVALID, [size, -1], [0, -1])
+
+
+def test_scales_refused():
+    call = lambda scale: rb.lib().rosaq_attend(CTX, C.byref(kv()), C.byref(batch()), ROWS, 256, 2, scale, 2 * ROWS, 256, 0, None)  # noqa: E731
+    for scale in (2.0 ** 58, -2.0 ** 58, 0.0, 1e-45):
+        assert call(scale) == rb.ROSAQ_OK, scale
+    for scale in (2.0 ** 58 * 1.001, -1e30, float("inf"), float("nan")):
+        assert call(scale) == INVALID, scale
