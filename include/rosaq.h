@@ -354,7 +354,8 @@ int rosaq_linear_static(rosaq_ctx *ctx, const void *x, int M, int64_t ldx, const
  *
  * The linears of a decoder layer above leave these to the caller in the paper; they are here so that a decoding step need not leave the
  * library.  Rows are fp16, one per token, heads next to each other (what rosaq_linear writes and rosaq_rotate reads); row strides in
- * elements, multiples of 8; pointers 16-byte aligned.  A call of no rows does nothing and returns ROSAQ_OK.
+ * elements, multiples of 8; pointers 16-byte aligned.  A call of no rows does nothing and returns ROSAQ_OK, with a batch
+ * of no sequences too.
  * What the DEVICE arrays of a batch say can only be checked on the device: rows, lengths and pages that do not fit are cut or left out so
  * that no access leaves the buffers, the status word becomes ROSAQ_ERR_INVALID_ARG (rosaq_last_status), and the results of the
  * sequences concerned are undefined.
@@ -428,7 +429,7 @@ int64_t rosaq_kv_page_bytes(int n_kv_heads, int head_dim, int bits, int page_tok
  *              sequence; they are read once for the whole batch.  kv_len and table do not count them.
  */
 typedef struct {
-  int32_t n_seqs;
+  int32_t n_seqs;          /* at least one, or none and no rows (the rest is not looked at) */
   int32_t ld_table;        /* row stride of the table; pages of a row * page_tokens <= 2^30 */
   const int32_t *row_start, *kv_len, *table;
   const int32_t *prefix_table;   /* prefix_tokens / page_tokens entries, rounded up */

@@ -34,6 +34,10 @@ int check_kv(const rosaq_kv *kv, KvView *out) {
 }
 
 int check_batch(const rosaq_kv_batch *b, const rosaq_kv *kv, int n_rows, KvBatchView *out) {
+  if (b && b->n_seqs == 0 && n_rows == 0) {         // nothing of it is looked at
+    *out = KvBatchView{};
+    return ROSAQ_OK;
+  }
   if (!b || b->n_seqs < 1 || b->ld_table < 1 || !b->row_start || !b->kv_len || !b->table) return ROSAQ_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(b->row_start) | reinterpret_cast<uintptr_t>(b->kv_len) | reinterpret_cast<uintptr_t>(b->table)) & 3)
     return ROSAQ_ERR_ALIGNMENT;
@@ -127,7 +131,7 @@ int rosaq_kv_locate(const rosaq_kv *kv, const rosaq_kv_batch *batch, int n_rows,
   int st = check_kv(kv, &view);
   if (st == ROSAQ_OK) st = check_batch(batch, kv, n_rows, &b);
   if (st == ROSAQ_OK && (n_rows < 0 || !offset || !slot)) st = ROSAQ_ERR_INVALID_ARG;
-  if (st != ROSAQ_OK) return st;
+  if (st != ROSAQ_OK || b.n_seqs == 0) return st;
   for (int i = 0; i < n_rows; ++i) offset[i] = slot[i] = -1;
   const int all = b.row_start[b.n_seqs], total = std::min(all, n_rows), bytes = kv_block_bytes(kv->head_dim, kv->bits);
   if (all > n_rows) st = ROSAQ_ERR_INVALID_ARG;

@@ -199,3 +199,14 @@ def test_scores_far_below_zero(ctx, new, scale):
     want = v[7].double().view(4, 1, 128).expand(4, 4, 128).reshape(1, -1).expand(new, -1)
     # (a read is rounded to fp16 too: half a step each, and what a scale's logarithm and reciprocal are off by)
     inside(out, want, 2 * 2.0 ** -11 * want.abs() + 2.0 ** -19 * 16)
+
+
+def test_a_step_of_no_sequences(ctx):
+    held, _ = filled(np.random.default_rng(29), 2, 64, 4, 16, [5])
+    kept = held.pages.clone()
+    empty = torch.empty((0, 2 * 64), dtype=torch.float16, device="cuda")
+    batch = rb.KvBatch(ints([0]), ints([]), torch.empty((0, 4), dtype=torch.int32, device="cuda"))
+    ctx.kv_write(held, batch, empty, empty)
+    assert ctx.kv_read(held, batch, 0)[1].shape == (0, 128) and ctx.attend(empty, held, batch).shape == (0, 128)
+    assert ctx.rope(empty, ints([]), ctx.rope_create(64)).shape == (0, 128)
+    assert ctx.last_status() == rb.ROSAQ_OK and torch.equal(held.pages, kept)

@@ -32,3 +32,15 @@ def test_scales_refused():
         assert call(scale) == rb.ROSAQ_OK, scale
     for scale in (2.0 ** 58 * 1.001, -1e30, float("inf"), float("nan")):
         assert call(scale) == INVALID, scale
+
+
+@pytest.mark.parametrize("name", ["rosaq_kv_write", "rosaq_kv_read", "rosaq_attend"])
+def test_batches_of_no_sequences(name):
+    none = dict(n_seqs=0, ld_table=0, row_start=None, kv_len=None, table=None)
+    assert rows_call(name, kv(), batch(**none), None, 256, None, 256, 0) == rb.ROSAQ_OK
+    assert rows_call(name, kv(), batch(n_seqs=0), ROWS, 256, 2 * ROWS, 256, 0) == rb.ROSAQ_OK
+    for n in (1, -1):
+        assert rows_call(name, kv(), batch(**none), ROWS, 256, 2 * ROWS, 256, n) == INVALID
+    assert rows_call(name, kv(), batch(n_seqs=-1), None, 256, None, 256, 0) == INVALID
+    offset, slot = C.c_int64(), C.c_int32()
+    assert rb.lib().rosaq_kv_locate(C.byref(kv()), C.byref(batch(**none)), 0, C.byref(offset), C.byref(slot)) == rb.ROSAQ_OK
