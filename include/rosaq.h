@@ -468,6 +468,10 @@ int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batc
 int rosaq_attend(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, const void *q, int64_t ldq, int n_q_heads, float scale,
                  void *out, int64_t ldo, int n_rows, void *stream);
 
+/* Test hook, host only (no GPU, no context; no array is read): which passes of such a call run on the kernel of many rows: 1 the one over the sequences,
+ * 2 the one over the prefix, 3 both, 0 none; or a negative status. */
+int rosaq_attend_forms(const rosaq_kv *kv, const rosaq_kv_batch *batch, int n_rows, int n_q_heads);
+
 #ifdef __cplusplus
 }
 #endif

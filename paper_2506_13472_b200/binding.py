@@ -25,6 +25,7 @@ EXPORTS = [
     "rosaq_plan_equal_shares", "rosaq_plan_create", "rosaq_plan_run", "rosaq_plan_free", "rosaq_plan_ctas",
     "rosaq_plan_schedule", "rosaq_set_plan_costs", "rosaq_set_plan_pairs", "rosaq_rope_create", "rosaq_rope_free", "rosaq_rope_apply",
     "rosaq_kv_page_bytes", "rosaq_kv_locate", "rosaq_kv_write", "rosaq_kv_read", "rosaq_attend",
+    "rosaq_attend_forms",
 ]
 ROPE_SCALING = {"plain": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 
@@ -117,6 +118,7 @@ def lib():
         L.rosaq_kv_locate.argtypes = [C.POINTER(_Kv), C.POINTER(_KvBatch), C.c_int, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
         L.rosaq_kv_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p]
         L.rosaq_kv_read.argtypes = L.rosaq_kv_write.argtypes
+        L.rosaq_attend_forms.argtypes = [C.POINTER(_Kv), C.POINTER(_KvBatch), C.c_int, C.c_int]
         L.rosaq_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float, C.c_void_p, C.c_int64,
                                    C.c_int, C.c_void_p]
         _lib = L
@@ -220,6 +222,15 @@ def kv_locate(row_start, kv_len, table, rows, n_pages, n_kv_heads, head_dim, bit
     offset, slot = (C.c_int64 * max(rows, 1))(), (C.c_int32 * max(rows, 1))()
     st = lib().rosaq_kv_locate(C.byref(kv), C.byref(b), rows, offset, slot)
     return st, list(offset)[:rows], list(slot)[:rows]
+
+
+def attend_forms(n_seqs, n_rows, n_q_heads, n_kv_heads, head_dim, pages_of_seq, page_tokens=64, bits=4, prefix_tokens=0):
+    """rosaq_attend_forms (host only) of a batch of those sizes, or RosaqError: 1 the sequences' pass on the kernel of many rows, 2 the prefix's, 3 both."""
+    kv, b = _Kv(16, 1, page_tokens, n_kv_heads, head_dim, bits), _KvBatch(n_seqs, pages_of_seq, 4, 4, 4, 4, prefix_tokens, 0)
+    st = lib().rosaq_attend_forms(C.byref(kv), C.byref(b), n_rows, n_q_heads)
+    if st < 0:
+        raise RosaqError(st, "rosaq_attend_forms")
+    return st
 
 
 class KvCache:

@@ -540,14 +540,22 @@ int launch_few(rosaq_ctx *ctx, AtParams p, cudaStream_t s) {
   return kv_launch(kern, dim3(ctas), C::kThreads, C::kSmem, s, p);
 }
 
-int launch_any(rosaq_ctx *ctx, int hd, int bits, const AtParams &p, long long rows_of_seq, cudaStream_t s) {
-  const long long room = p.prefix_tokens > 0 ? p.prefix_tokens : (long long)p.b.width * (kKvBlock << p.kv.page_shift);
-  if (rows_of_seq >= kManyRows && (double)rows_of_seq * p.b.n_seqs * p.kv.n_heads * (double)room >= (double)kManyWork) return launch_attend_rows(ctx, p, hd, bits, s);
+int launch_any(rosaq_ctx *ctx, int hd, int bits, const AtParams &p, bool many, cudaStream_t s) {
+  if (many) return launch_attend_rows(ctx, p, hd, bits, s);
   if (hd == 128) return bits == 4 ? launch_few<128, 4>(ctx, p, s) : launch_few<128, 8>(ctx, p, s);
   return bits == 4 ? launch_few<64, 4>(ctx, p, s) : launch_few<64, 8>(ctx, p, s);
 }
 
 }  // namespace
+
+int attend_forms(const KvView &kv, const KvBatchView &b, int prefix_tokens, int n_q_heads) {
+  const long long group = n_q_heads / kv.n_heads;
+  auto many = [&](long long rows_of_seq, int n_seqs, long long room) {
+    return rows_of_seq >= kManyRows && (double)rows_of_seq * n_seqs * kv.n_heads * (double)room >= (double)kManyWork;
+  };
+  const bool own = many(((long long)b.n_rows + b.n_seqs - 1) / b.n_seqs * group, b.n_seqs, (long long)b.width * (kKvBlock << kv.page_shift));
+  return (own ? 1 : 0) + (prefix_tokens > 0 && many(b.n_rows * group, 1, prefix_tokens) ? 2 : 0);
+}
 
 int launch_attend(rosaq_ctx *ctx, const KvView &kv, int hd, int bits, const KvBatchView &b, const int32_t *prefix_table, int prefix_tokens,
                   const __half *q, long long ldq, int n_q_heads, float scale, __half *out, long long ldo, cudaStream_t s) {
@@ -560,17 +568,17 @@ int launch_attend(rosaq_ctx *ctx, const KvView &kv, int hd, int bits, const KvBa
   if (prefix_bytes) st = grow_workspace(ctx, reinterpret_cast<void **>(&ctx->at_prefix), &ctx->at_prefix_bytes, prefix_bytes);
   if (st != ROSAQ_OK) return st;
   p.arrived = ctx->at_arrived;
-  const long long rows_of_seq = ((long long)b.n_rows + b.n_seqs - 1) / b.n_seqs * p.group;
+  const int forms = attend_forms(kv, b, prefix_tokens, n_q_heads);
   if (prefix_tokens > 0) {
     p.prefix = ctx->at_prefix;
     AtParams f = p;
     f.prefix_tokens = prefix_tokens, f.last_row = b.n_seqs;
     f.b.n_seqs = 1, f.b.table = prefix_table;
     f.b.ld_table = f.b.width = (int)(((long long)prefix_tokens + (kKvBlock << kv.page_shift) - 1) / (kKvBlock << kv.page_shift));
-    st = launch_any(ctx, hd, bits, f, (long long)b.n_rows * p.group, s);
+    st = launch_any(ctx, hd, bits, f, forms & 2, s);
     if (st != ROSAQ_OK) return st;
   }
-  return launch_any(ctx, hd, bits, p, rows_of_seq, s);
+  return launch_any(ctx, hd, bits, p, forms & 1, s);
 }
 
 }  // namespace rosaq

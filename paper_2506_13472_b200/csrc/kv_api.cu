@@ -185,6 +185,17 @@ int rosaq_kv_read(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batc
                         static_cast<cudaStream_t>(stream));
 }
 
+int rosaq_attend_forms(const rosaq_kv *kv, const rosaq_kv_batch *batch, int n_rows, int n_q_heads) {
+  KvView view;
+  KvBatchView b;
+  int st = check_kv(kv, &view);
+  if (st == ROSAQ_OK) st = check_batch(batch, kv, n_rows, &b);
+  if (st != ROSAQ_OK) return st;
+  if (n_rows < 0 || n_q_heads < 1 || batch->prefix_tokens < 0) return ROSAQ_ERR_INVALID_ARG;
+  if (n_q_heads % kv->n_kv_heads != 0) return ROSAQ_ERR_UNSUPPORTED_SHAPE;
+  return n_rows == 0 ? 0 : attend_forms(view, b, batch->prefix_tokens, n_q_heads);
+}
+
 int rosaq_attend(rosaq_ctx *ctx, const rosaq_kv *kv, const rosaq_kv_batch *batch, const void *q, int64_t ldq, int n_q_heads, float scale,
                  void *out, int64_t ldo, int n_rows, void *stream) {
   if (!ctx || n_q_heads < 1) return ROSAQ_ERR_INVALID_ARG;

@@ -136,6 +136,7 @@ int launch_kv_write(const KvView &kv, int hd, int bits, const KvBatchView &b, co
                     int *status, cudaStream_t s);
 int launch_kv_read(const KvView &kv, int hd, int bits, const KvBatchView &b, __half *k, long long ldk, __half *v, long long ldv, int *status,
                    cudaStream_t s);
+int attend_forms(const KvView &kv, const KvBatchView &b, int prefix_tokens, int n_q_heads);   // which passes run on attend_rows.cu: the sequences' own (1), the prefix (2)
 int launch_attend(rosaq_ctx *ctx, const KvView &kv, int hd, int bits, const KvBatchView &b, const int32_t *prefix_table, int prefix_tokens,
                   const __half *q, long long ldq, int n_q_heads, float scale, __half *out, long long ldo, cudaStream_t s);
 
