@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2506_13472_b200 import binding as rb
-from tests import kv_reference as ref
+from tests import kv_reference as ref, test_gpu_kv_attention as gpu
 from tests.test_gpu_kv_attention import expect, fill, filled, inside, ints, same
 
 pytestmark = pytest.mark.gpu
@@ -210,3 +210,98 @@ def test_a_step_of_no_sequences(ctx):
     assert ctx.kv_read(held, batch, 0)[1].shape == (0, 128) and ctx.attend(empty, held, batch).shape == (0, 128)
     assert ctx.rope(empty, ints([]), ctx.rope_create(64)).shape == (0, 128)
     assert ctx.last_status() == rb.ROSAQ_OK and torch.equal(held.pages, kept)
+
+
+def updates(heads, group, lens, new, prefix=0):
+    """Additions to one accumulator, at most: one per sixteen tokens of a CTA's share, which is an equal one or 16 chunks of 64 tokens."""
+    return 128 + sum((n + prefix) // 16 * -(-m * group // 8) for n, m in zip(lens, new)) * heads // 148
+
+
+@pytest.mark.parametrize("heads,group,hd,bits,page,lens,new,prefix,room", [(*c, 0, False) for c in gpu.CASES] + [(*c, 0, True) for c in gpu.MANY] + [
+    (8, 4, 128, 4, 64, [i % 40 + 1 for i in range(64)], [1] * 64, 2500, False),
+    (2, 8, 64, 8, 16, [30, 9, 400], [3, 9, 20], 333, False),
+    (1, 3, 128, 8, 32, [40], [40], 40000, False),
+    (2, 8, 64, 4, 16, [3, 1, 0, 70, 9], [3, 1, 0, 30, 9], 9001, False),
+    (2, 2, 64, 8, 64, [33000], [2], 0, False),
+    (2, 2, 64, 8, 64, [33000], [40], 0, False),
+])
+def test_errors_by_norm(ctx, heads, group, hd, bits, page, lens, new, prefix, room):
+    """Every row and head of long contexts, whose results are small beside the values that they are made of."""
+    rng = np.random.default_rng(30)
+    all_lens = [prefix] + lens
+    held, table = filled(rng, heads, hd, bits, page, all_lens)
+    fill(ctx, rng, held, table, all_lens, loud=3.0)
+    pre, table = ints(table[0].tolist()), table[1:]
+    if room:
+        width = -(-(1 << 22) // (-(-sum(new) // len(lens)) * group * len(lens) * heads * page))
+        table = np.pad(table, ((0, 0), (0, max(0, width - table.shape[1]))), constant_values=-5)
+    q = torch.from_numpy(rng.standard_normal((sum(new), heads * group * hd)).astype(np.float16)).cuda()
+    out = ctx.attend(q, held, rb.KvBatch(starts(new), ints(lens), ints(table.tolist()), prefix=(pre, prefix) if prefix else None))
+    assert ctx.last_status() == rb.ROSAQ_OK
+    args, at = (held.pages, heads, hd, bits, page), 0
+    shared = ref.values(*args, pre, prefix) if prefix else None
+    for i, (n, m) in enumerate(zip(lens, new)):
+        if m == 0:
+            continue
+        kv = ref.values(*args, ints(table[i].tolist()), n)
+        if shared:
+            kv = [[torch.cat([a, b]) for a, b in zip(x, y)] for x, y in zip(shared, kv)]
+        seen = torch.arange(prefix + n, device="cuda")[None, :] < prefix + n - m + 1 + torch.arange(m, device="cuda")[:, None]
+        want, bound = ref.attention_norm(q[at:at + m].double().view(m, -1, hd), kv, seen, hd ** -0.5, updates(heads, group, lens, new, prefix))
+        off = (out[at:at + m].double().view(m, -1, hd) - want).norm(dim=-1)
+        assert bool((off <= bound).all()), (i, float((off / bound).max()))
+        at += m
+
+
+@pytest.mark.parametrize("heads,group,hd,bits,page,lens,new,prefix,many", [
+    (1, 4, 128, 4, 1024, [70000], [1], 0, 0),                               # one tile over all CTAs
+    (2, 1, 128, 8, 64, [9000, 5000, 20000], [1, 1, 1], 0, 0),
+    (8, 1, 64, 4, 64, [6000] * 5, [2] * 5, 0, 0),
+    (1, 2, 128, 4, 1024, [70000], [100], 0, 1),
+    (4, 4, 128, 8, 64, [9000, 20000], [30, 50], 0, 1),
+    (2, 2, 64, 4, 64, [40000], [300], 0, 1),
+    (2, 4, 128, 4, 64, [4500] * 30, [3] * 30, 16001, 2),
+    (2, 4, 128, 8, 64, [5000, 4200], [1, 1], 9001, 0),
+])
+def test_no_part_is_lost(ctx, heads, group, hd, bits, page, lens, new, prefix, many):
+    """Every 32 tokens have a value of 3 in one channel and nothing elsewhere, about alike in weight: a part that is missing or counts twice is a seventeenth
+    or more of that channel's result, where roundings are a 300th."""
+    rng = np.random.default_rng(31)
+    all_lens = [prefix or 16] + lens
+    held, table = filled(rng, heads, hd, bits, page, all_lens)
+    assert rb.attend_forms(len(lens), sum(new), heads * group, heads, hd, table.shape[1], page, bits, prefix) == many
+    k = torch.randn((sum(all_lens), heads * hd), device="cuda").half()
+    at = torch.cat([torch.arange(n, device="cuda") for n in all_lens]) // 32 % hd
+    v = 3.0 * (at[:, None, None] == torch.arange(hd, device="cuda")).half().expand(-1, heads, -1).reshape(-1, heads * hd)
+    ctx.kv_write(held, rb.KvBatch(starts(all_lens), ints(all_lens), ints(table.tolist())), k, v)
+    q = (0.3 * torch.randn((sum(new), heads * group * hd), device="cuda")).half()
+    pre = (ints(table[0].tolist()), prefix) if prefix else None
+    out = ctx.attend(q, held, rb.KvBatch(starts(new), ints(lens), ints(table[1:].tolist()), prefix=pre))
+    assert ctx.last_status() == rb.ROSAQ_OK
+    want, _ = expect(held, table[1:], lens, new, q, hd ** -0.5, pre)
+    # All terms of a channel have one sign: the weights' 11 bits in product and sum, the result's rounding, and, of codes about their middle, what accumulators that hold up to the
+    # middle times a scale cut off
+    middle = 3.0 / ref.QMAX[bits] * (10 if bits == 4 else 128)
+    inside(out, want, 3 * 2.0 ** -11 * want + updates(heads, group, lens, new, prefix) * 2.0 ** -23 * middle + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("new,bits", [(1, 4), (1, 8), (16, 4), (16, 8)])
+def test_waits_that_run_out(ctx, new, bits):
+    """One poll per wait, and more chunks than any warp has slots for: the launch ends and says so, and the next call is as ever."""
+    rng = np.random.default_rng(32)
+    lens = [70000]
+    held, table = filled(rng, 8, 128, bits, 64, lens)
+    fill(ctx, rng, held, table, lens)
+    assert rb.attend_forms(1, new, 32, 8, 128, table.shape[1]) == (1 if new > 1 else 0)
+    q = torch.randn((new, 32 * 128), device="cuda").half()
+    batch = rb.KvBatch(starts([new]), ints(lens), ints(table.tolist()))
+    want = ctx.attend(q, held, batch).clone()
+    limit = ctx.set_wait_limit(1)
+    status = []
+    for _ in range(5):
+        ctx.attend(q, held, batch)
+        status.append(ctx.last_status())
+    ctx.set_wait_limit(limit)
+    assert rb.ROSAQ_ERR_TIMEOUT in status and set(status) <= {rb.ROSAQ_OK, rb.ROSAQ_ERR_TIMEOUT}
+    for _ in range(2):
+        assert same(ctx.attend(q, held, batch), want) and ctx.last_status() == rb.ROSAQ_OK
