@@ -305,3 +305,70 @@ def test_waits_that_run_out(ctx, new, bits):
     assert rb.ROSAQ_ERR_TIMEOUT in status and set(status) <= {rb.ROSAQ_OK, rb.ROSAQ_ERR_TIMEOUT}
     for _ in range(2):
         assert same(ctx.attend(q, held, batch), want) and ctx.last_status() == rb.ROSAQ_OK
+
+
+@pytest.mark.parametrize("lens,new,prefix,many", [([3], [20], 0, 0), ([3], [20], 40, 0), ([10, 600, 0], [700, 640, 5], 0, 1), ([0, 300], [600, 400], 4100, 3)])
+def test_more_rows_than_tokens(ctx, lens, new, prefix, many):
+    """The first rows of such a sequence see nothing but the prefix, whole tiles of them too: zeros, or the prefix alone."""
+    rng = np.random.default_rng(33)
+    held, table = filled(rng, 2, 128, 4, 64, [max(prefix, 16)] + lens)
+    fill(ctx, rng, held, table, [max(prefix, 16)] + lens)
+    pre, table = (ints(table[0].tolist()), prefix) if prefix else None, np.pad(table[1:], ((0, 0), (0, 60 if many else 0)), constant_values=-5)
+    assert rb.attend_forms(len(lens), sum(new), 4, 2, 128, table.shape[1], 64, 4, prefix) == many
+    q = torch.randn((sum(new), 4 * 128), device="cuda").half()
+    out = torch.full_like(q, 7.0)
+    ctx.attend(q, held, rb.KvBatch(starts(new), ints(lens), ints(table.tolist()), prefix=pre), out=out)
+    assert ctx.last_status() == rb.ROSAQ_OK
+    args, at = (held.pages, 2, 128, 4, 64), 0
+    for i, (n, m) in enumerate(zip(lens, new)):
+        kv = [[x[:n] for x in y] for y in ref.values(*args, ints(table[i].tolist()), max(n, 1))]
+        if pre:
+            kv = [[torch.cat([a, b]) for a, b in zip(x, y)] for x, y in zip(ref.values(*args, *pre), kv)]
+        # (the prefix is seen by all: a sequence that is too short takes nothing away from it)
+        t = torch.arange(prefix + n, device="cuda")[None, :]
+        seen = (t < prefix) | (t - prefix < n - m + 1 + torch.arange(m, device="cuda")[:, None])
+        want, bound = ref.attention(q[at:at + m].double().view(m, 4, 128), kv, seen, 128 ** -0.5)
+        if prefix + n:                                        # (of nothing: zeros, seen to below)
+            inside(out[at:at + m].view(m, 4, 128), want, bound, i)
+        at += m
+    if not prefix:
+        blind = torch.cat([torch.arange(m) < m - n for n, m in zip(lens, new)]).cuda()
+        assert blind.any() and torch.all(out[blind] == 0)
+
+
+def test_caches_past_four_gigabytes(ctx):
+    """Pages whose bytes lie past 32 bits, and a table of pages in no order over all of them: as in a small cache of the same pages."""
+    rng = np.random.default_rng(34)
+    heads, lens = 32, [700, 333, 64]
+    size = rb.kv_page_bytes(heads, 128, 8, 64)
+    n_pages = (9 << 30) // size
+    small = rb.KvCache(torch.zeros((22, size), dtype=torch.uint8, device="cuda"), heads, 128, 8, 64)
+    big = rb.KvCache(torch.empty((n_pages, size), dtype=torch.uint8, device="cuda"), heads, 128, 8, 64)
+    places = rng.choice(n_pages, 22, replace=False)
+    places[:3] = n_pages - 1, (1 << 32) // size, (1 << 33) // size
+    table = np.full((3, 11), -5)
+    at = 0
+    for i, n in enumerate(lens):
+        need = -(-n // 64)
+        table[i, :need], at = np.arange(at, at + need), at + need
+    pre = np.arange(at, at + 3)
+    far = np.where(table < 0, -5, places[table])
+    big.pages[torch.tensor(places, device="cuda")] = small.pages
+    k, v = (torch.randn((sum(lens) + 150, heads * 128), device="cuda").half() for _ in range(2))
+    q = torch.randn((sum(lens), heads * 128), device="cuda").half()
+    outs = []
+    for held, t, p in ((small, table, pre), (big, far, places[pre])):
+        p = ints(p.tolist())
+        ctx.kv_write(held, rb.KvBatch(ints([0, 150]), ints([150]), p[None]), k[:150], v[:150])
+        tab = ints(t.tolist())
+        batch = rb.KvBatch(starts(lens), ints(lens), tab)
+        ctx.kv_write(held, batch, k[150:], v[150:])
+        got = list(ctx.kv_read(held, batch, sum(lens)))
+        for rows in (1, 64):                                  # decoding and many rows, behind a prefix
+            got.append(ctx.attend(q[:3 * rows], held, rb.KvBatch(starts([rows] * 3), ints(lens), tab, prefix=(p, 150))))
+        outs.append(got)
+        assert ctx.last_status() == rb.ROSAQ_OK
+    assert torch.equal(big.pages[torch.tensor(places, device="cuda")], small.pages)
+    for a, b in zip(*outs):
+        assert same(a, b)
+    assert float(outs[0][2].abs().max()) > 0.1
