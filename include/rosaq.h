@@ -385,7 +385,8 @@ int rosaq_rope_free(rosaq_rope *r);
 /*
  * y[n_rows][ldy] = the n_heads heads of every row of x[n_rows][ldx] turned by the row's position: with t = positions[row] f_i,
  *   a' = magnitude (a cos t - b sin t),  b' = magnitude (b cos t + a sin t)   for the pairs (a, b), fp32, rounded once to fp16.
- *   positions  DEVICE int32 [n_rows]; any value, a negative one turns back.  The angle is exact to 2^-33 turns for all of them.
+ *   positions  DEVICE int32 [n_rows]; any value, a negative one turns back.  Position times f_i (f_i a double) is reduced to one turn in integers, off by 2^-33 turns at
+ *              most, and rounded to an fp32 number of radians, off by less than 2^-23 turns
  *   y          may be x (same stride); any other overlap is ROSAQ_ERR_INVALID_ARG
  * q and k next to each other in one buffer are one call.
  */

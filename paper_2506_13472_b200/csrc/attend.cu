@@ -12,9 +12,10 @@
 // Tokens are the rows of the first MMA (m16n8k16: 16 tokens x 8 query rows) and the k of the second one (16 channels x 8 query rows), so a group of
 // up to eight query heads costs no more than one, and a lane's words of a block (kv_common.cuh) are its A fragments in both.
 //
-// Bound: memory for one row per sequence and long contexts at 8 bits (16 x 32768 tokens of 8 heads of 128: 0.94 of the copy bandwidth); at 4 bits the instructions, about 480 per pair
-// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 136 us, 119 without the
-// arithmetic, 95 at the copy bandwidth.  Short calls are bound by latency: 5.7 us for one chunk, 0.9 to 1.0 us per further chunk of a warp, 5 us to join CTAs.
+// Bound: memory for one row per sequence and long contexts at 8 bits (16 sequences of 20000 to 32767 tokens, 8 heads of 128: 0.93 of the copy bandwidth); at 4 bits the instructions, about 484 per pair
+// of blocks of 16 tokens and one key/value head (4352 bytes, head of 128), of which a scheduler issues one in two cycles: 64 x 2250 tokens, 32 heads, take 133 us, 119 without the
+// arithmetic, 95 at the copy bandwidth.  With one query head per key/value head seven of an MMA's eight columns are empty, and half of the softmax's instructions work on a column that always is.
+// Short calls are bound by latency: 5.7 us for one chunk, 1.0 to 1.3 us per further chunk of a warp, 5 us to join CTAs.
 // The list of (sequence, head, tile of query rows, chunk) is cut into equal shares, one per CTA, whatever the lengths: CTAs read lengths on the device, so a captured launch
 // follows them.  A CTA's share is cut into one run per warp, each with slots of its own, all filled by one more warp, a lane per slot (warps that fill their own: 153 to 168 us
 // instead of 152).  A tile whose chunks several CTAs share is finished by the CTA that arrives last, in the order of the shares: no CTA waits for another, and the bits are the
@@ -30,8 +31,8 @@ constexpr int kChunk = 2, kTokens = kChunk * kKvBlock;   // blocks that a warp t
 constexpr int kRows = 8;                            // query rows of a tile
 // From kManyRows query rows per sequence and key/value head on, and from kManyWork of (row, key/value head, token that the table has room for) in all: attend_rows.cu, which takes 10 us
 // more for any call and a third to a half of the time per row and token.  (us here and there, 32 query and 8 key/value heads of 128 at 4 bits: 32 rows of each of 16 sequences of 1000
-// tokens 34 and 35, 64 rows 47 and 37; of one sequence of 500 tokens 64 rows 12 and 24; of 4000 tokens 64 rows 26 and 25, 128 rows 32 and 26; of 30000 tokens 64 rows 65 and 50;
-// 128 rows behind a prefix of 500 tokens 21 and 32, of 4000 40 and 36, of 16000 76 and 46.)
+// tokens 34 and 36, 64 rows 47 and 38; of one sequence of 500 tokens 64 rows 12 and 24; of 4000 tokens 64 rows 26 and 25, 128 rows 33 and 26; of 30000 tokens 64 rows 67 and 52;
+// 128 rows behind a prefix of 500 tokens 20 and 32, of 4000 40 and 35, of 16000 77 and 47.)
 constexpr long long kManyRows = 64, kManyWork = 1ll << 22;
 // Greatest wait limit.  A warp that gives up leaves others to give up by themselves, so every wait has to end in a time that somebody can wait for; and some poll 32 times as often.
 constexpr long long kMostPolls = 1ll << 24;
@@ -66,7 +67,8 @@ struct Cfg {
   static constexpr int kStageBytes = kChunk * kv_block_bytes(kHd, kBits);
   static constexpr int kThreads = 32 * (kWarps + 1);
   // Two CTAs on an SM: at 4 bits 14 warps with 128 registers, at 8 bits ten with two slots each.  More warps with fewer registers that compute one block at a time are slower:
-  // 64 x 2250 tokens 141 us, 20 warps with 96 registers 157, 24 with 80 183 to 197.
+  // 64 x 2250 tokens 141 us when this was measured, 20 warps with 96 registers 157, 24 with 80 183 to 197.  (The instance of heads of 128 at 4 bits needs a little more than 128: by
+  // -Xptxas -v it spills 8 bytes and loads 20.)
   static constexpr int kPerSm = 2;
   static constexpr int kAccLd = kHd + 4;            // floats: two rows of a pair on different banks
   static constexpr int kPartBytes = kRows * (4 * kAccLd + 16);   // a part of a tile: [row][kAccLd], then [row]{maximum, sum, sum of least values, -}

@@ -112,9 +112,9 @@ __device__ __forceinline__ void settle(const AtParams &p, Cursor &c) {
 __device__ __forceinline__ long long divide(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
 // How the list is cut.  Even shares, except that
-//   - tiles of few chunks are not cut where there is no need: joining the parts of several CTAs takes about 5 us, a chunk of a warp 0.9 (one sequence of 333 tokens, 32
-//     heads: 13.8 us in 50 shares of seven chunks, 8.7 in 32 shares of a tile), and
-//   - where all tiles are short, a cut moves to the nearer end of the tile it falls into: then there is nothing to join (64 x 200 tokens, 32 heads: 34.6 and 19.8 us).
+//   - tiles of few chunks are not cut where there is no need: joining the parts of several CTAs takes about 5 us, a chunk of a warp 1.0 (one sequence of 333 tokens, 32
+//     heads: 13.9 us in 50 shares of seven chunks, 9.9 in 32 shares of a tile), and
+//   - where all tiles are short, a cut moves to the nearer end of the tile it falls into: then there is nothing to join (64 x 200 tokens, 32 heads: 29.9 and 21.0 us).
 struct Shares {
   long long total, part;                            // part = total / ctas, and what is left
   int ctas, left, near;

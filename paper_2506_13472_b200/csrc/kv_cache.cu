@@ -10,8 +10,8 @@
 // blocks leave as 16-byte stores; into those that begin or end inside a block the bytes of the other tokens are read first (bytes stored one by one would be 190 partial
 // sectors per token and head, 64 x 32 of them 6.9 us).  One warp of a call writes to a block, so nothing comes between.
 //
-// Measured (heads of 128): 2048 rows of 32 heads at 4 bits written in 12.1 us, read in 8.2 (floor 6.5 each way), 13200 rows of 40 heads read in 67 (floor 55);
-// 64 single rows of 32 heads written in 5.0, a launch's latency.
+// Measured (heads of 128): 2048 rows of 32 heads at 4 bits written in 12.6 us, read in 8.5 (floor 6.5 each way); 13200 rows of 40 heads read in 63 to 73 (343 MB, floor 55: four fifths are
+// writes, of which a fill kernel does 3.9 TB/s, 69 us for this much); 64 single rows of 32 heads written in 5.5, latency of lengths, table, rows and quantizer in turn.
 #include "kv_common.cuh"
 
 namespace rosaq {
@@ -107,7 +107,7 @@ __device__ __forceinline__ void write_block(bool value, const KvPiece &p, const 
   __syncwarp();
   uint8_t *const params = block + 2 * kv_code_bytes(kHd, kBits) + (value ? 4 * kKvBlock : 0);
   // ---- codes in the values' place.  Four lanes per token, each every fourth 16 bytes: what a token costs besides its values (two divisions, the exchange) is shared by 32
-  // of them (2048 rows x 32 heads: 15.9 us with sixteen lanes per token)
+  // of them (2048 rows x 32 heads: 12.6 us, with sixteen lanes per token 15.9)
   const int quad = lane & 3;
 #pragma unroll 1
   for (int t0 = p.slot & ~7; t0 < p.slot + p.n; t0 += 8) {

@@ -4,10 +4,11 @@
 //
 // Angles: position * f_i in fp32 would be off by 0.06 radians at a million positions, so the host gives f_i as a 64-bit fraction of a turn;
 // the integer product with the position is the angle modulo one turn, off by 2^-33 turns at most, and its upper 32 bits, as a signed number,
-// go to sincosf with no range left to reduce.  A negative position turns back.
+// go to sincosf with no range left to reduce (as an fp32 number of radians: up to half a turn, off by less than 2^-23 turns).  A negative position turns back.
 //
-// Bound: memory.  A thread holds 16 channels of a head, works out their angles once and walks over the heads of its row.  Measured: 8191 rows of 40 heads of 128 in
-// 35 us (168 MB, 4.8 TB/s; the copy of that size takes 57 through a library), 64 rows of 64 heads in 2.9.
+// Bound: memory, and waves of CTAs that do not fill it.  A thread holds 16 channels of a head, works out their angles once and walks over the heads of its row.  Measured: 8191 rows of
+// 40 heads of 128 in 35.4 us (168 MB, 4.7 TB/s; an elementwise kernel takes 28.7 over as much, the floor at the copy bandwidth is 25.6): the grid is made for eight CTAs per SM, registers
+// admit four, so that these 1024 CTAs are 1.7 waves, and a thread's first loads wait for eight sines and cosines.  64 rows of 64 heads: 2.9 us.
 #include <algorithm>
 
 #include "kv_common.cuh"
