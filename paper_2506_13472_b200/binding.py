@@ -256,7 +256,7 @@ class KvBatch:
             assert t.is_cuda and t.dtype is torch.int32 and t.stride(-1) == 1 and t.get_device() == kv_len.get_device()
         assert row_start.dim() == kv_len.dim() == 1 and row_start.numel() == n + 1 and table.dim() == 2 and table.shape[0] == n
         assert n <= 1 or table.stride(0) >= table.shape[1] > 0
-        assert prefix is None or prefix[0].dim() == 1
+        assert prefix is None or prefix[0].is_contiguous()
         self.row_start, self.kv_len, self.table, self.prefix, self.device = row_start, kv_len, table, prefix, kv_len.get_device()
         self._s = _KvBatch(n, table.shape[1] if n == 1 else table.stride(0), row_start.data_ptr(), kv_len.data_ptr(), table.data_ptr(),
                            None if prefix is None else prefix[0].data_ptr(), 0 if prefix is None else int(prefix[1]), table.shape[1])
@@ -449,7 +449,7 @@ class Context:
         n, ldq = _act(q)
         heads, rest = divmod(q.shape[1], cache.head_dim)
         assert rest == 0 and q.get_device() == cache.device == batch.device == self.device
-        assert batch.prefix is None or batch.prefix[0].shape[0] * cache.page_tokens >= batch.prefix[1]   # (as many pages as the tokens need are looked at)
+        assert batch.prefix is None or batch.prefix[0].numel() * cache.page_tokens >= batch.prefix[1]   # (as many pages as the tokens need are looked at)
         if out is None:
             out = q.new_empty(q.shape)
         assert out.shape == q.shape and out.dtype is torch.float16 and out.stride(1) == 1 and out.get_device() == self.device
