@@ -140,7 +140,7 @@ def attention_norm(q, kv, seen, scale, updates=128):
       2 * 2^-11 S                    the weights' 11 bits, the same in products and sums.  Each is off by at most 2^-11 and by 0.42 * 2^-11 in the mean square (an
                                      error uniform in half a step either way, a mantissa of logarithmic density): nearly five deviations, and for up to four tokens the worst case
       updates 2^-23 * 4 (|out| + S)  accumulators: each update cuts off less than 2^-23 of what they hold, a walk of no more than some S
-      2^-20 (1 + m) sum w |v - out|  scores, as in attention()
+      2 * 2^-20 (1 + m) S            scores: an error of up to 2^-20 (1 + m), as in attention(), is one of the weight, and has as little to do with the value as the weight's rounding
     and half a step of a subnormal result per channel."""
     (kc, kl, _), (vc, vl, _) = kv
     n, hq, hd = q.shape
@@ -154,7 +154,7 @@ def attention_norm(q, kv, seen, scale, updates=128):
     size = out.norm(dim=-1)
     away = (v.pow(2).sum(-1).T[None] - 2 * torch.einsum("nhd,thd->nht", out, v) + size[..., None] ** 2).clamp(min=0)
     s = (w ** 2 * away).sum(-1).sqrt()
-    bound = 2.0 ** -11 * (size + 2 * s) + updates * 2.0 ** -21 * (size + s) + 2.0 ** -20 * (1 + m) * (w * away.sqrt()).sum(-1) + 2.0 ** -25 * hd ** 0.5
+    bound = 2.0 ** -11 * (size + 2 * s) + updates * 2.0 ** -21 * (size + s) + 2.0 ** -19 * (1 + m) * s + 2.0 ** -25 * hd ** 0.5
     return out, bound
 
 
